@@ -455,6 +455,114 @@ int mslt_op_attention_lse_bwd(const void* d_qkv, const void* d_ctx, const float*
                               void* cuda_stream, int32_t sync);
 
 /*
+ * Rotary positions for query and key heads (an alternative to the position table "emb.pos" of the encoder; the paper
+ * leaves the encoder to BERT, Section 4.1).  For row t at position P, head h and pair i of the rot_dim / 2 pairs of a
+ * head, with a = 2 pi frac(P turns[i] / 2^64) and m = magnitude:
+ *     y[u] = m (x[u] cos a - x[w] sin a),   y[w] = m (x[u] sin a + x[w] cos a)
+ * where (u, w) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) with interleaved = 1.  Elements rot_dim..head_dim of a head
+ * are copied.  inverse = 1 turns back (sin a negated): the gradient of the call with inverse = 0.  The angle is formed
+ * in 64-bit integers, so it is as exact at position 2^31 as at 1.  y may be x itself with the same strides, or
+ * memory that does not overlap it.
+ */
+typedef struct {
+  int32_t dtype;                  /* 0: fp32, 1: bf16                                                    */
+  int32_t rows, heads, head_dim;  /* head_dim a multiple of 8, <= 128                                    */
+  const void* x;                  /* device; element (t, h, e) at x + t * x_row + h * x_head + e         */
+  int64_t x_row, x_head;          /* elements; multiples of 16 bytes, as is the address                  */
+  void* y;                        /* device, likewise                                                    */
+  int64_t y_row, y_head;
+  const int32_t* positions;       /* device [rows], any int32; NULL: row t is at position t % seq        */
+  int32_t seq;                    /* rows of a sequence, used where positions is NULL                    */
+  int32_t rot_dim;                /* a multiple of 8 in [8, head_dim]; the normalising calls also take 0 */
+  int32_t interleaved;
+  const uint64_t* turns;          /* device [rot_dim / 2], from mslt_rope_turns, 16-byte aligned         */
+  float magnitude;
+  int32_t inverse;                /* mslt_op_rope only                                                   */
+} mslt_rope_desc;
+int mslt_op_rope(const mslt_rope_desc* desc, void* cuda_stream, int32_t sync);
+
+/*
+ * The table that mslt_op_rope reads: for pair i the turns a position, f_i / (2 pi) as a 64-bit binary fraction, with
+ * f_i = base^(-2 i / rot_dim) radians, adapted to contexts `factor` times as long as the trained one:
+ *   scaling 0  f_i as it is (factor 1)
+ *   scaling 1  f_i / factor: positions are interpolated
+ *   scaling 2  the base is multiplied by factor^(rot_dim / (rot_dim - 2)), so that the slowest pair is interpolated
+ *   scaling 3  by parts: a pair that makes r = trained_len f_i / (2 pi) turns over the trained length keeps
+ *              g = clamp((r - 1) / 31, 0, 1) of f_i and takes 1 - g of f_i / factor; *magnitude is 0.1 ln(factor) + 1
+ * host_turns: host [rot_dim / 2]; magnitude: host, 1 for scaling 0 to 2.  Runs on the host and needs no device.
+ */
+int mslt_rope_turns(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t trained_len,
+                    uint64_t* host_turns, float* magnitude);
+
+/*
+ * Normalisation of every query and key head with the rotation above in the same pass: n = gain (x - mean) / sqrt(var +
+ * eps) + bias over the head_dim elements of a head with center = 1, n = gain x / sqrt(mean(x^2) + eps) + bias with
+ * center = 0, then y = rotation of n.  Heads [0, q_heads) take row 0 of gain and bias, heads [q_heads, heads) row 1.
+ * The backward call takes the forward's x again, forms the statistics from it, and writes dx, d_dgain and, where not
+ * NULL, d_dbias (written, not added to; sums in a fixed order: the same bits on every run).  dx may be dy itself with the
+ * same strides.  d_scratch: device, 16-byte aligned, of mslt_op_qk_norm_rope_bwd_scratch_bytes bytes; contents on entry
+ * do not matter.
+ */
+typedef struct {
+  mslt_rope_desc rope;   /* x, y as in mslt_op_rope (the backward call does not use y); inverse must be 0; rot_dim may be 0 */
+  int32_t q_heads;       /* in [0, rope.heads] */
+  int32_t center;
+  float eps;             /* > 0 */
+  const float* gain;     /* device [2, head_dim], 16-byte aligned */
+  const float* bias;     /* device [2, head_dim] or NULL */
+  const void* dy;        /* backward: device, element (t, h, e) at dy + t * dy_row + h * dy_head + e */
+  int64_t dy_row, dy_head;
+  void* dx;
+  int64_t dx_row, dx_head;
+  float* dgain;          /* backward: device [2, head_dim], 16-byte aligned */
+  float* dbias;          /* backward: device [2, head_dim] or NULL */
+} mslt_qk_norm_desc;
+int mslt_op_qk_norm_rope(const mslt_qk_norm_desc* desc, void* cuda_stream, int32_t sync);
+size_t mslt_op_qk_norm_rope_bwd_scratch_bytes(int32_t rows, int32_t heads, int32_t head_dim);
+int mslt_op_qk_norm_rope_bwd(const mslt_qk_norm_desc* desc, void* d_scratch, size_t scratch_bytes, void* cuda_stream,
+                             int32_t sync);
+
+/*
+ * Attention of S queries and S keys a sequence under a mask, for any S, with what mslt_op_attention has no place for:
+ * query heads that share keys, documents packed into a row, causal and prefix masks, a bias by distance, capped scores.
+ *     z_ij = scale q_i . k_j;   cap > 0: z_ij = cap tanh(z_ij / cap);   slopes: z_ij -= slopes[h] |i - j|
+ *     query i sees key j where  i < len and j < len  (lens),  docs[i] == docs[j]  (docs),  and
+ *                               j <= i or j < prefix  (causal; without prefix: j <= i)
+ *     ctx_i = sum_j softmax_j(z_ij) v_j over the keys that query i sees, lse_i = ln sum_j e^(z_ij)
+ * A query that sees no key gets ctx 0, lse -infinity and no gradient.  Query head h reads key head h / (heads / kv_heads).
+ * Rows at or beyond a sequence's length take no part, whatever they hold (NaN too).
+ * bf16: probabilities (relative to the row's maximum) are rounded to bf16 before the product with v, and the row is
+ * divided by the sum of what was rounded.  `rest` (bf16, ctx's strides) receives what rounding took off ctx; given to the
+ * backward call it makes the rows of the scores' gradient sum to zero also where the keys have much in common.
+ * Backward: the gradients of ctx by q, k and v from dctx, ctx, lse (and rest) of the forward call; dk and dv are summed over
+ * the query heads that share them, in a fixed order.  The slopes are constants and have no gradient.
+ */
+typedef struct {
+  void* data;                 /* device; element (b, i, h, e) at data + b * batch + i * row + h * head + e */
+  int64_t batch, row, head;   /* elements; multiples of 16 bytes, as is the address                        */
+} mslt_heads;
+typedef struct {
+  int32_t dtype;                                  /* 0: fp32, 1: bf16                          */
+  int32_t B, S, heads, kv_heads, head_dim;        /* head_dim a multiple of 8, <= 128; heads a multiple of kv_heads; S <= 131072 */
+  mslt_heads q, k, v, ctx;                        /* inputs and output of the forward call      */
+  void* rest;                                     /* dtype 1: ctx's layout, or NULL              */
+  float* lse;                                     /* device [B, heads, S]; forward: may be NULL  */
+  mslt_heads dctx, dq, dk, dv;                    /* backward call                               */
+  float scale, cap;                               /* cap 0: none                                 */
+  const float* slopes;                            /* device [heads] or NULL                      */
+  int32_t causal;
+  const int32_t* prefix;                          /* device [B] or NULL; needs causal            */
+  const int32_t* docs;                            /* device [B, S] or NULL; any values           */
+  const int32_t* lens;                            /* device [B] or NULL (all S)                  */
+} mslt_attention_desc;
+/* d_status and sync as in mslt_op_attention. */
+int mslt_op_attention_masked(const mslt_attention_desc* desc, int32_t* d_status, void* cuda_stream, int32_t sync);
+/* d_scratch: device, 16-byte aligned; contents on entry do not matter. */
+size_t mslt_op_attention_masked_bwd_scratch_bytes(int32_t B, int32_t S, int32_t heads);
+int mslt_op_attention_masked_bwd(const mslt_attention_desc* desc, void* d_scratch, size_t scratch_bytes, int32_t* d_status,
+                                 void* cuda_stream, int32_t sync);
+
+/*
  * mslt_op_cross_entropy without any device allocation by anybody.  (The paper has no counterpart
  * of this call; it exists for the integration below.)
  *

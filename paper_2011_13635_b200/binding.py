@@ -48,6 +48,35 @@ class GemmDesc(C.Structure):
                 ("residual", C.c_void_p), ("split_k", C.c_int32), ("seq_lens", C.c_void_p)]
 
 
+class RopeDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("rows", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
+                ("x", C.c_void_p), ("x_row", C.c_int64), ("x_head", C.c_int64),
+                ("y", C.c_void_p), ("y_row", C.c_int64), ("y_head", C.c_int64),
+                ("positions", C.c_void_p), ("seq", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("turns", C.c_void_p), ("magnitude", C.c_float), ("inverse", C.c_int32)]
+
+
+class QkNormDesc(C.Structure):
+    _fields_ = [("rope", RopeDesc), ("q_heads", C.c_int32), ("center", C.c_int32), ("eps", C.c_float),
+                ("gain", C.c_void_p), ("bias", C.c_void_p),
+                ("dy", C.c_void_p), ("dy_row", C.c_int64), ("dy_head", C.c_int64),
+                ("dx", C.c_void_p), ("dx_row", C.c_int64), ("dx_head", C.c_int64),
+                ("dgain", C.c_void_p), ("dbias", C.c_void_p)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class AttentionDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("B", C.c_int32), ("S", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("q", Heads), ("k", Heads), ("v", Heads), ("ctx", Heads),
+                ("rest", C.c_void_p), ("lse", C.c_void_p),
+                ("dctx", Heads), ("dq", Heads), ("dk", Heads), ("dv", Heads),
+                ("scale", C.c_float), ("cap", C.c_float), ("slopes", C.c_void_p), ("causal", C.c_int32),
+                ("prefix", C.c_void_p), ("docs", C.c_void_p), ("lens", C.c_void_p)]
+
+
 EXPORTS = ["mslt_query_bytes", "mslt_create", "mslt_destroy", "mslt_add_layers", "mslt_set_trainable",
            "mslt_set_optimizer", "mslt_step", "mslt_step_nsp", "mslt_step_backward", "mslt_step_apply", "mslt_num_grad_buckets",
            "mslt_grad_bucket", "mslt_set_bucket_hook", "mslt_read_loss", "mslt_forward", "mslt_num_layers",
@@ -60,6 +89,9 @@ EXPORTS = ["mslt_query_bytes", "mslt_create", "mslt_destroy", "mslt_add_layers",
            "mslt_op_cross_entropy_scratch_bytes", "mslt_op_cross_entropy_noalloc", "mslt_op_layernorm",
            "mslt_op_layernorm_bwd", "mslt_op_softmax", "mslt_op_softmax_bwd", "mslt_op_colsum",
            "mslt_op_attention", "mslt_op_attention_bwd", "mslt_op_attention_lse", "mslt_op_attention_lse_bwd",
+           "mslt_rope_turns", "mslt_op_rope", "mslt_op_qk_norm_rope", "mslt_op_qk_norm_rope_bwd",
+           "mslt_op_qk_norm_rope_bwd_scratch_bytes", "mslt_op_attention_masked", "mslt_op_attention_masked_bwd",
+           "mslt_op_attention_masked_bwd_scratch_bytes",
            "mslt_debug_starve_next_gemm", "mslt_debug_starve_next_attention", "mslt_debug_check_guards",
            "mslt_debug_set_gemm_variant", "mslt_debug_last_gemm_form", "mslt_debug_gemm_in_step"]
 
@@ -135,6 +167,17 @@ lib.mslt_op_attention_lse.argtypes = [_P, _P, _P, C.c_int32, C.c_int32, C.c_int3
 lib.mslt_op_attention_lse_bwd.argtypes = [_P, _P, _P, _P, _P, _P, C.c_int32, C.c_int32, C.c_int32, C.c_float, _P, _P,
                                           C.c_int32]
 lib.mslt_op_colsum.argtypes = [C.c_int32, _P, C.c_int64, C.c_int32, C.c_int32, _P, _P, C.c_int32]
+
+lib.mslt_rope_turns.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_int32, _P, C.POINTER(C.c_float)]
+lib.mslt_op_rope.argtypes = [C.POINTER(RopeDesc), _P, C.c_int32]
+lib.mslt_op_qk_norm_rope.argtypes = [C.POINTER(QkNormDesc), _P, C.c_int32]
+lib.mslt_op_qk_norm_rope_bwd.argtypes = [C.POINTER(QkNormDesc), _P, C.c_size_t, _P, C.c_int32]
+lib.mslt_op_qk_norm_rope_bwd_scratch_bytes.restype = C.c_size_t
+lib.mslt_op_qk_norm_rope_bwd_scratch_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+lib.mslt_op_attention_masked.argtypes = [C.POINTER(AttentionDesc), _P, _P, C.c_int32]
+lib.mslt_op_attention_masked_bwd.argtypes = [C.POINTER(AttentionDesc), _P, C.c_size_t, _P, _P, C.c_int32]
+lib.mslt_op_attention_masked_bwd_scratch_bytes.restype = C.c_size_t
+lib.mslt_op_attention_masked_bwd_scratch_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
 
 
 class MsltError(RuntimeError):
@@ -275,6 +318,179 @@ def mslt_op_colsum(x, n: int, out, stream: int, sync: bool = True) -> None:
     """out[:n] += x[:, :n].sum(0); x [rows, ld] float or bf16, out fp32."""
     _check(lib.mslt_op_colsum(_dt(x), x.data_ptr(), x.stride(0), x.shape[0], n, out.data_ptr(),
                               C.c_void_p(stream), int(sync)))
+
+
+# -- positions and masks of the encoder's attention -------------------------------------------------
+# These take views (any strides that are multiples of 16 bytes, elements of a head side by side) and check what the
+# library cannot see: shapes, types, devices.
+
+def _refuse(what: str, text: str):
+    raise MsltError(-1, f"{what}: {text}")
+
+
+def _same(what: str, ref, shape, dtype=None, **tensors):
+    """Each tensor (None passes) has this shape and type, lies on ref's device, and ends in neighbouring elements."""
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if tuple(t.shape) != tuple(shape):
+            _refuse(what, f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+        if t.dtype != (dtype or ref.dtype):
+            _refuse(what, f"{name} is {t.dtype}, needs {dtype or ref.dtype}")
+        if t.device != ref.device:
+            _refuse(what, f"{name} is on {t.device}, needs {ref.device}")
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            _refuse(what, f"the last dimension of {name} must be contiguous")
+
+
+def _table(what: str, ref, shape, dtype, **tensors):
+    """As _same, and contiguous."""
+    _same(what, ref, shape, dtype, **tensors)
+    for name, t in tensors.items():
+        if t is not None and not t.is_contiguous():
+            _refuse(what, f"{name} must be contiguous")
+
+
+def _call(ref, fn, *args):
+    """Runs fn with ref's device current: a stream belongs to its device."""
+    import torch
+    if ref.device.index == torch.cuda.current_device():
+        _check(fn(*args))
+    else:
+        with torch.cuda.device(ref.device):
+            _check(fn(*args))
+
+
+def _float_or_bf16(what: str, name: str, t, dims: int):
+    import torch
+    if t.dim() != dims or t.dtype not in (torch.float32, torch.bfloat16):
+        _refuse(what, f"{name} needs {dims} dimensions and float32 or bfloat16")
+    if not t.is_cuda:
+        raise MsltError(-4, f"{what}: {name} is not on a CUDA device: this library has no CPU path")
+
+
+ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
+
+
+def mslt_rope_turns(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained_len: int = 512):
+    """(numpy uint64 [rot_dim / 2], magnitude): the table of mslt_op_rope, which takes it as an int64 CUDA tensor
+    (`torch.from_numpy(turns.view(numpy.int64)).cuda()`), and the factor of long contexts."""
+    if scaling not in ROPE_SCALING:
+        _refuse("rope_turns", f"scaling must be one of {sorted(ROPE_SCALING)}")
+    turns = np.zeros(max(1, rot_dim // 2), dtype=np.uint64)
+    m = C.c_float()
+    _check(lib.mslt_rope_turns(rot_dim, base, ROPE_SCALING[scaling], factor, trained_len, turns.ctypes.data, C.byref(m)))
+    return turns, m.value
+
+
+def _rope_desc(what, x, y, turns, positions, seq, interleaved, magnitude, inverse) -> RopeDesc:
+    import torch
+    _float_or_bf16(what, "x", x, 3)
+    rows, heads, dim = x.shape
+    _same(what, x, x.shape, y=y)
+    rot = 0 if turns is None else 2 * turns.shape[0]
+    if turns is not None:
+        _table(what, x, (rot // 2,), torch.int64, turns=turns)
+    _table(what, x, (rows,), torch.int32, positions=positions)
+    return RopeDesc(_dt(x), rows, heads, dim, x.data_ptr(), x.stride(0), x.stride(1), _ptr(y), 0 if y is None else y.stride(0),
+                    0 if y is None else y.stride(1), _ptr(positions), seq, rot, int(interleaved), _ptr(turns), magnitude, int(inverse))
+
+
+def mslt_op_rope(x, y, turns, stream: int, positions=None, seq: int = 0, interleaved: bool = False, magnitude: float = 1.0,
+                 inverse: bool = False, sync: bool = True) -> None:
+    """x, y [rows, heads, head_dim] float or bf16 (y may be x); turns int64 [rot_dim / 2] from mslt_rope_turns;
+    positions int32 [rows] or None (row t at t % seq): CUDA tensors."""
+    d = _rope_desc("rope", x, y, turns, positions, seq, interleaved, magnitude, inverse)
+    _call(x, lib.mslt_op_rope, C.byref(d), stream, int(sync))
+
+
+def _norm_desc(what, x, y, gain, turns, q_heads, eps, bias, center, positions, seq, interleaved, magnitude) -> QkNormDesc:
+    import torch
+    rope = _rope_desc(what, x, y, turns, positions, seq, interleaved, magnitude, False)
+    _table(what, x, (2, x.shape[2]), torch.float32, gain=gain, bias=bias)
+    return QkNormDesc(rope, q_heads, int(center), eps, gain.data_ptr(), _ptr(bias))
+
+
+def mslt_op_qk_norm_rope(x, y, gain, turns, q_heads: int, eps: float, stream: int, bias=None, center: bool = False, positions=None,
+                         seq: int = 0, interleaved: bool = False, magnitude: float = 1.0, sync: bool = True) -> None:
+    """x, y, positions as in mslt_op_rope (turns None: no rotation); gain, bias fp32 [2, head_dim]: row 0 for the first
+    q_heads heads, row 1 for the others; bias may be None."""
+    d = _norm_desc("qk_norm_rope", x, y, gain, turns, q_heads, eps, bias, center, positions, seq, interleaved, magnitude)
+    if y is None:
+        _refuse("qk_norm_rope", "y is None")
+    _call(x, lib.mslt_op_qk_norm_rope, C.byref(d), stream, int(sync))
+
+
+def mslt_op_qk_norm_rope_bwd_scratch_bytes(rows: int, heads: int, head_dim: int) -> int:
+    return lib.mslt_op_qk_norm_rope_bwd_scratch_bytes(rows, heads, head_dim)
+
+
+def mslt_op_qk_norm_rope_bwd(dy, x, dx, gain, dgain, turns, q_heads: int, eps: float, scratch, stream: int, dbias=None,
+                             center: bool = False, positions=None, seq: int = 0, interleaved: bool = False,
+                             magnitude: float = 1.0, sync: bool = True) -> None:
+    """dy, x, dx [rows, heads, head_dim] (dx may be dy); x is the forward's input; dgain, dbias (or None) fp32
+    [2, head_dim] are written; scratch uint8."""
+    import torch
+    what = "qk_norm_rope_bwd"
+    d = _norm_desc(what, x, None, gain, turns, q_heads, eps, None, center, positions, seq, interleaved, magnitude)
+    _same(what, x, x.shape, dy=dy, dx=dx)
+    _table(what, x, (2, x.shape[2]), torch.float32, dgain=dgain, dbias=dbias)
+    _table(what, x, scratch.shape, torch.uint8, scratch=scratch)
+    d.dy, d.dy_row, d.dy_head = dy.data_ptr(), dy.stride(0), dy.stride(1)
+    d.dx, d.dx_row, d.dx_head = dx.data_ptr(), dx.stride(0), dx.stride(1)
+    d.dgain, d.dbias = dgain.data_ptr(), _ptr(dbias)
+    _call(x, lib.mslt_op_qk_norm_rope_bwd, C.byref(d), scratch.data_ptr(), scratch.numel(), stream, int(sync))
+
+
+def _heads(t) -> Heads:
+    return Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def _attention_desc(what, q, k, v, ctx, lse, status, scale, cap, slopes, causal, prefix, docs, lens, rest) -> AttentionDesc:
+    import torch
+    _float_or_bf16(what, "q", q, 4)
+    B, S, heads, dim = q.shape
+    _same(what, q, (B, S, k.shape[2] if k.dim() == 4 else 0, dim), k=k, v=v)
+    _same(what, q, q.shape, ctx=ctx, rest=rest)
+    if rest is not None and rest.stride() != ctx.stride():
+        _refuse(what, "rest must have the strides of ctx")
+    _table(what, q, (B, heads, S), torch.float32, lse=lse)
+    _table(what, q, (heads,), torch.float32, slopes=slopes)
+    _table(what, q, (B,), torch.int32, prefix=prefix, lens=lens)
+    _table(what, q, (B, S), torch.int32, docs=docs)
+    _table(what, q, (1,), torch.int32, status=status)
+    d = AttentionDesc(_dt(q), B, S, heads, k.shape[2], dim, _heads(q), _heads(k), _heads(v), _heads(ctx), _ptr(rest), _ptr(lse))
+    d.scale, d.cap, d.causal = scale, cap, int(causal)
+    d.slopes, d.prefix, d.docs, d.lens = _ptr(slopes), _ptr(prefix), _ptr(docs), _ptr(lens)
+    return d
+
+
+def mslt_op_attention_masked(q, k, v, ctx, lse, scale: float, status, stream: int, cap: float = 0.0, slopes=None,
+                             causal: bool = False, prefix=None, docs=None, lens=None, rest=None, sync: bool = True) -> None:
+    """q, ctx [B, S, heads, head_dim], k, v [B, S, kv_heads, head_dim] float or bf16; lse fp32 [B, heads, S] or None;
+    slopes fp32 [heads], prefix and lens int32 [B], docs int32 [B, S], rest bf16 like ctx: CUDA tensors or None."""
+    d = _attention_desc("attention_masked", q, k, v, ctx, lse, status, scale, cap, slopes, causal, prefix, docs, lens, rest)
+    _call(q, lib.mslt_op_attention_masked, C.byref(d), status.data_ptr(), stream, int(sync))
+
+
+def mslt_op_attention_masked_bwd_scratch_bytes(B: int, S: int, heads: int) -> int:
+    return lib.mslt_op_attention_masked_bwd_scratch_bytes(B, S, heads)
+
+
+def mslt_op_attention_masked_bwd(q, k, v, ctx, lse, dctx, dq, dk, dv, scratch, scale: float, status, stream: int, cap: float = 0.0,
+                                 slopes=None, causal: bool = False, prefix=None, docs=None, lens=None, rest=None,
+                                 sync: bool = True) -> None:
+    """The other arguments as in mslt_op_attention_masked (ctx, lse and rest are its results); dctx, dq like q, dk, dv
+    like k; scratch uint8."""
+    import torch
+    what = "attention_masked_bwd"
+    d = _attention_desc(what, q, k, v, ctx, lse, status, scale, cap, slopes, causal, prefix, docs, lens, rest)
+    _same(what, q, q.shape, dctx=dctx, dq=dq)
+    _same(what, q, k.shape, dk=dk, dv=dv)
+    _table(what, q, scratch.shape, torch.uint8, scratch=scratch)
+    d.dctx, d.dq, d.dk, d.dv = _heads(dctx), _heads(dq), _heads(dk), _heads(dv)
+    _call(q, lib.mslt_op_attention_masked_bwd, C.byref(d), scratch.data_ptr(), scratch.numel(), status.data_ptr(), stream,
+          int(sync))
 
 
 class Mslt:

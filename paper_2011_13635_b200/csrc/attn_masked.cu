@@ -1,0 +1,94 @@
+// Entry points of attention under masks: checks of the arguments and the choice of the kernels by type.
+#include "attn_masked.h"
+
+#include <math.h>
+
+#include "op_check.h"
+
+using namespace mslt;
+
+namespace {
+
+int check_heads(const char* what, const char* name, const mslt_heads& h, int dtype) {
+  const int unit = dtype == 1 ? 8 : 4;
+  if (!h.data) return op_refuse(MSLT_ERR_ARG, "%s: %s is null", what, name);
+  if ((uintptr_t)h.data & 15) return op_refuse(MSLT_ERR_ARG, "%s: %s must be 16-byte aligned", what, name);
+  if (h.batch < 0 || h.row < 0 || h.head < 0 || h.batch % unit || h.row % unit || h.head % unit)
+    return op_refuse(MSLT_ERR_ARG, "%s: strides of %s must be multiples of 16 bytes", what, name);
+  return 0;
+}
+
+int check_attention(const char* what, const mslt_attention_desc* d, const int32_t* status) {
+  if (!d || !status) return op_refuse(MSLT_ERR_ARG, "%s: null pointer", what);
+  if (d->dtype != 0 && d->dtype != 1) return op_refuse(MSLT_ERR_ARG, "%s: dtype must be 0 or 1", what);
+  if (d->B < 1 || d->S < 1 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads)
+    return op_refuse(MSLT_ERR_ARG, "%s: needs B, S, heads >= 1 and heads a multiple of kv_heads", what);
+  if (d->head_dim < 8 || d->head_dim > 128 || d->head_dim % 8)
+    return op_refuse(MSLT_ERR_ARG, "%s: head_dim must be a multiple of 8 in [8, 128]", what);
+  if (d->S > 131072 || (int64_t)d->B * d->heads * d->S > 0x7fffffffll)
+    return op_refuse(MSLT_ERR_SIZE, "%s: at most 131072 rows a sequence and 2^31 - 1 rows of all heads", what);
+  if (!isfinite(d->scale) || !isfinite(d->cap) || d->cap < 0)
+    return op_refuse(MSLT_ERR_ARG, "%s: scale and cap must be finite, cap not negative", what);
+  if (d->prefix && !d->causal) return op_refuse(MSLT_ERR_ARG, "%s: a prefix needs causal", what);
+  if (d->dtype == 0 && d->rest) return op_refuse(MSLT_ERR_ARG, "%s: rest is for dtype 1", what);
+  if ((uintptr_t)d->rest & 15) return op_refuse(MSLT_ERR_ARG, "%s: rest must be 16-byte aligned", what);
+  int rc = 0;
+  if ((rc = check_heads(what, "q", d->q, d->dtype)) || (rc = check_heads(what, "k", d->k, d->dtype)) ||
+      (rc = check_heads(what, "v", d->v, d->dtype)) || (rc = check_heads(what, "ctx", d->ctx, d->dtype)))
+    return rc;
+  return 0;
+}
+
+int end_attention(const char* what, const int32_t* status, cudaStream_t st, int sync) {
+  int rc = op_end(what, st, sync);
+  if (rc || !sync) return rc;
+  int h = 0;
+  if (cudaMemcpy(&h, status, 4, cudaMemcpyDeviceToHost) != cudaSuccess)
+    return op_refuse(MSLT_ERR_CUDA, "%s: reading the status word failed", what);
+  if (h & 1) return op_refuse(MSLT_ERR_DEVICE, "%s: a bounded wait ran out on the device", what);
+  return 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+int mslt_op_attention_masked(const mslt_attention_desc* desc, int32_t* d_status, void* cuda_stream, int32_t sync) {
+  const char* what = "attention_masked";
+  int rc = check_attention(what, desc, d_status);
+  if (rc || (rc = op_need_device())) return rc;
+  return op_nothrow(what, [&] {
+    char err[256] = "";
+    int r = attn_masked_f32_fwd(*desc, (cudaStream_t)cuda_stream, err);
+    if (r) return op_refuse(r, "%s", err);
+    return end_attention(what, d_status, (cudaStream_t)cuda_stream, sync);
+  });
+}
+
+size_t mslt_op_attention_masked_bwd_scratch_bytes(int32_t B, int32_t S, int32_t heads) {
+  if (B < 1 || S < 1 || heads < 1) return 0;
+  return ((size_t)B * S * heads * sizeof(float) + 255) / 256 * 256;
+}
+
+int mslt_op_attention_masked_bwd(const mslt_attention_desc* desc, void* d_scratch, size_t scratch_bytes, int32_t* d_status,
+                                 void* cuda_stream, int32_t sync) {
+  const char* what = "attention_masked_bwd";
+  int rc = check_attention(what, desc, d_status);
+  if (rc) return rc;
+  if ((rc = check_heads(what, "dctx", desc->dctx, desc->dtype)) || (rc = check_heads(what, "dq", desc->dq, desc->dtype)) ||
+      (rc = check_heads(what, "dk", desc->dk, desc->dtype)) || (rc = check_heads(what, "dv", desc->dv, desc->dtype)))
+    return rc;
+  if (!desc->lse) return op_refuse(MSLT_ERR_ARG, "%s: lse is null", what);
+  const size_t need = mslt_op_attention_masked_bwd_scratch_bytes(desc->B, desc->S, desc->heads);
+  if (!d_scratch || scratch_bytes < need || ((uintptr_t)d_scratch & 15))
+    return op_refuse(MSLT_ERR_SIZE, "%s: scratch must be 16-byte aligned and hold %zu bytes", what, need);
+  if ((rc = op_need_device())) return rc;
+  return op_nothrow(what, [&] {
+    char err[256] = "";
+    int r = attn_masked_f32_bwd(*desc, (float*)d_scratch, (cudaStream_t)cuda_stream, err);
+    if (r) return op_refuse(r, "%s", err);
+    return end_attention(what, d_status, (cudaStream_t)cuda_stream, sync);
+  });
+}
+
+}  // extern "C"
