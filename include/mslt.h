@@ -328,7 +328,8 @@ int mslt_op_gemm_f32_split(const mslt_gemm_desc* desc, void* d_scratch, size_t s
  */
 int mslt_debug_starve_next_gemm(int32_t on);
 /* The same hook for the fused attention kernels: the NEXT mslt_op_attention / mslt_op_attention_bwd
- * call (or attention launch inside a step) runs with an idle producer and a 20 ms wait limit. */
+ * call, dtype-1 call of mslt_op_attention_masked or its backward, or attention launch inside a step runs with an
+ * idle producer and a 20 ms wait limit. */
 int mslt_debug_starve_next_attention(int32_t on);
 
 /*

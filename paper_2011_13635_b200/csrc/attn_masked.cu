@@ -59,7 +59,8 @@ int mslt_op_attention_masked(const mslt_attention_desc* desc, int32_t* d_status,
   if (rc || (rc = op_need_device())) return rc;
   return op_nothrow(what, [&] {
     char err[256] = "";
-    int r = attn_masked_f32_fwd(*desc, (cudaStream_t)cuda_stream, err);
+    int r = desc->dtype == 1 ? attn_masked_tc_fwd(*desc, d_status, (cudaStream_t)cuda_stream, err)
+                             : attn_masked_f32_fwd(*desc, (cudaStream_t)cuda_stream, err);
     if (r) return op_refuse(r, "%s", err);
     return end_attention(what, d_status, (cudaStream_t)cuda_stream, sync);
   });
@@ -85,7 +86,8 @@ int mslt_op_attention_masked_bwd(const mslt_attention_desc* desc, void* d_scratc
   if ((rc = op_need_device())) return rc;
   return op_nothrow(what, [&] {
     char err[256] = "";
-    int r = attn_masked_f32_bwd(*desc, (float*)d_scratch, (cudaStream_t)cuda_stream, err);
+    int r = desc->dtype == 1 ? attn_masked_tc_bwd(*desc, (float*)d_scratch, d_status, (cudaStream_t)cuda_stream, err)
+                             : attn_masked_f32_bwd(*desc, (float*)d_scratch, (cudaStream_t)cuda_stream, err);
     if (r) return op_refuse(r, "%s", err);
     return end_attention(what, d_status, (cudaStream_t)cuda_stream, sync);
   });

@@ -1944,6 +1944,7 @@ attn_delta_kernel(const bf16* __restrict__ c, const bf16* __restrict__ dc, float
 static std::atomic<long long> g_attn_launches{0};
 static std::atomic<int> g_attn_starve{0};
 void attn_starve_next(int on) { g_attn_starve.store(on ? 1 : 0); }
+bool attn_take_starve() { return g_attn_starve.exchange(0) != 0; }
 long long attn_launches() { return g_attn_launches.load(); }
 
 namespace {

@@ -284,6 +284,49 @@ def test_same_bits_on_every_run_and_in_a_graph(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dim,kw", [(64, {}), (64, dict(slopes=True, causal=True)), (128, dict(cap=15.0))])
+def test_every_block_of_a_large_launch_ends(dim, kw):
+    """Thousands of blocks with loops of all lengths, several times: a wait that misses its phase would run out (the call
+    raises then), and one that is let through too early changes results between runs."""
+    import torch
+    s = make("bf16", 8, 2048, 12, 4, dim, docs=documents(8, 2048, 6), lens=[2048, 2000, 1, 64, 700, 2047, 1999, 129], **kw)
+    first = run(s)
+    for _ in range(5):
+        again = run(s)
+        for k in first:
+            assert torch.equal(first[k], again[k]), k
+    # the first six query heads of the first sequence by themselves: context and dq to the bit
+    m = s["mask"]
+    few = {k: v if not torch.is_tensor(v) else v[:6] if k == "slopes" else v[:1] for k, v in m.items()}
+    got = run(dict(s, q=s["q"][:1, :, :6], dc=s["dc"][:1, :, :6], k=s["k"][:1, :, :2], v=s["v"][:1, :, :2], mask=few))
+    for k in ("ctx", "dq"):
+        assert torch.equal(got[k], first[k][:1, :, :6]), k
+
+
+@pytest.mark.gpu
+def test_a_wait_that_runs_out_is_reported():
+    """The producer of the next launch issues no copies: status after 20 ms, and the device stays usable."""
+    import torch
+    from paper_2011_13635_b200 import binding as B
+    s = make("bf16", 2, 300, 4, 2, 64)
+    want = run(s)
+    B.lib.mslt_debug_starve_next_attention(1)
+    with pytest.raises(B.MsltError) as e:
+        run(s, backward=False)
+    assert e.value.code == -5
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    grads = [torch.empty_like(s[k]) for k in ("q", "k", "v")]
+    scratch = torch.empty(B.mslt_op_attention_masked_bwd_scratch_bytes(2, 300, 4), dtype=torch.uint8, device="cuda")
+    B.lib.mslt_debug_starve_next_attention(1)
+    with pytest.raises(B.MsltError) as e:
+        B.mslt_op_attention_masked_bwd(s["q"], s["k"], s["v"], want["ctx"], want["lse"], s["dc"], *grads, scratch, s["scale"], status,
+                                       _stream())
+    assert e.value.code == -5
+    again = run(s)
+    assert all(torch.equal(again[k], want[k]) for k in want)
+
+
+@pytest.mark.gpu
 def test_two_streams_at_once():
     """Two calls that may run side by side, each with its own scratch."""
     import torch
