@@ -5,14 +5,17 @@
 // One pass: a head is read once, its statistics are sums over the few lanes that hold it, and the backward forms them
 // again from x instead of reading them.  Bound by HBM: 2 (rope, norm) or 3 (backward) passes over the heads.
 //
-// A lane holds 16 bytes of a head, the next power of two of lanes a head, so a warp has 32 / lanes heads of one row at a
-// time.  The angle of a pair depends on row and pair only: a warp works up to four such groups of heads with one set of
-// cosines and sines, and asks for all of their bytes before it forms them.  Angles: the table holds turns a position as
-// 64-bit fractions, position times table modulo 2^64 is the turn's fraction without any rounding that grows with the
-// position, and its upper 32 bits go to the sine.  In bf16 the sine is the hardware's (absolute error 2^-21 on
-// [-pi, pi], an eighth of a thousandth of the result's rounding 2^-9); in fp32 the library's sincospif.
-// Pairs at distance rot / 2 exchange their values through shuffles.  rot is a multiple of 8, so that distance is a number
-// of four-element quads and a lane's quads each come from one lane.
+// A lane holds two pieces of W elements of a head such that both elements of every pair are its own: pieces half a rotation
+// apart, or side by side where neighbours are paired (and the rest of the head likewise).  So nothing is exchanged but
+// the norm's sums, and the lane's pairs are W neighbours of the table in either layout.  W is 4 in either type: 8 bf16 a
+// piece measure the same for the rotation alone (19.0 against 19.1 us at 16384 rows x 24 heads x 64) and leave the norm's
+// backward too few registers (77 against 55 us).  The angle of a pair depends on row and pair only: a warp works three
+// groups of heads of a row with one set of cosines and sines, asks for all of their bytes before it forms them, and takes
+// the three sums of a norm side by side.  (One 16-byte piece a lane and the partner's values through shuffles: twice the
+// sines, 32 us.)  Angles: the table holds turns a position as 64-bit fractions, position times table modulo 2^64 is the turn's
+// fraction without any rounding that grows with the position, and its upper 32 bits go to the sine.  In bf16 the sine is
+// the hardware's (absolute error 2^-21 on [-pi, pi], an eighth of a thousandth of the result's rounding 2^-9); in fp32
+// the library's sincospif.
 #include <math.h>
 
 #include "common.cuh"
@@ -22,7 +25,6 @@ namespace mslt {
 namespace {
 
 constexpr int RO_WARPS = 8;
-constexpr int RO_PASSES = 4;         // groups of heads that a warp has under way
 constexpr int RO_MAX_BLOCKS = 1184;  // blocks of the backward pass that leave partial sums
 
 struct RotaryParams {
@@ -37,6 +39,33 @@ struct RotaryParams {
   float magnitude, sign, eps;
 };
 
+constexpr int W = 4;  // elements of a piece
+
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+  typedef float4 Raw;
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[W]) { VecT<float>::unpack(r, v); }
+  static __device__ __forceinline__ void store(float* p, const float (&v)[W]) { VecT<float>::store(p, v); }
+};
+template <> struct Piece<bf16> {
+  typedef uint2 Raw;
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[W]) {
+    const uint32_t w[2] = {r.x, r.y};
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ void store(bf16* p, const float (&v)[W]) {
+    uint2 r;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&r);
+    h[0] = __floats2bfloat162_rn(v[0], v[1]);
+    h[1] = __floats2bfloat162_rn(v[2], v[3]);
+    *reinterpret_cast<uint2*>(p) = r;
+  }
+};
+
 __device__ __forceinline__ void turn_of(int pos, uint64_t turns, bool exact, float& s, float& c) {
   const int32_t f = (int32_t)(((uint64_t)(int64_t)pos * turns) >> 32);
   const float t = (float)f * 2.3283064365386963e-10f;  // 2^-32: in [-1/2, 1/2)
@@ -49,178 +78,243 @@ __device__ __forceinline__ void turn_of(int pos, uint64_t turns, bool exact, flo
   }
 }
 
-__device__ __forceinline__ float lanes_sum(float v, int log_lanes) {
-  for (int o = (1 << log_lanes) >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
+// Sums over the lanes of a head, of all passes side by side
+template <int N>
+__device__ __forceinline__ void lanes_sum(float (&v)[N], int lanes) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    if (o < lanes) {
+#pragma unroll
+      for (int k = 0; k < N; k++) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    }
 }
 
-// v <- c v + s (partner of v): the rotation, with the sign of each element's side in s
-template <int V, bool INTER>
-__device__ __forceinline__ void rotate(float (&v)[V], const float (&c)[V], const float (&s)[V], const int (&src)[V / 4], bool odd) {
-  float w[V];
+// The lane's pairs turned: (a_j, b_j), or the neighbours in a and in b.  What does not turn is left as it is.
+template <bool INTER>
+__device__ __forceinline__ void rotate(float (&a)[W], float (&b)[W], const float (&c)[W], const float (&s)[W], bool turn_a, bool turn_b) {
   if (INTER) {
 #pragma unroll
-    for (int j = 0; j < V; j++) w[j] = v[j ^ 1];
-  } else {
-#pragma unroll
-    for (int q = 0; q < V / 4; q++)
-#pragma unroll
-      for (int j = 0; j < 4; j++) {
-        // an odd distance in quads: the partner lies in the other quad of its lane
-        const float give = V == 8 && odd ? v[(4 * q + j) ^ (V - 4)] : v[4 * q + j];
-        w[4 * q + j] = __shfl_sync(0xffffffffu, give, src[q]);
+    for (int j = 0; j < W / 2; j++) {
+      if (turn_a) {
+        const float u = a[2 * j], w = a[2 * j + 1];
+        a[2 * j] = fmaf(-w, s[j], u * c[j]);
+        a[2 * j + 1] = fmaf(u, s[j], w * c[j]);
       }
-  }
+      if (turn_b) {
+        const float u = b[2 * j], w = b[2 * j + 1], cb = c[W / 2 + j], sb = s[W / 2 + j];
+        b[2 * j] = fmaf(-w, sb, u * cb);
+        b[2 * j + 1] = fmaf(u, sb, w * cb);
+      }
+    }
+  } else if (turn_a) {
 #pragma unroll
-  for (int j = 0; j < V; j++) v[j] = fmaf(s[j], w[j], c[j] * v[j]);
+    for (int j = 0; j < W; j++) {
+      const float u = a[j], w = b[j];
+      a[j] = fmaf(-w, s[j], u * c[j]);
+      b[j] = fmaf(u, s[j], w * c[j]);
+    }
+  }
 }
 
-// OP 0: rotation, 1: norm and rotation, 2: backward of 1
-template <typename T, bool INTER, int OP>
-__global__ void __launch_bounds__(32 * RO_WARPS, 2)
-rotary_kernel(const RotaryParams p) {
-  constexpr int V = VecT<T>::N, NT = INTER ? V / 2 : V;
-  constexpr bool kExact = sizeof(T) == 4;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int lanes = 1 << p.log_lanes, g = lane & (lanes - 1), e = g * V;
-  const int sub = lane >> p.log_lanes, together = 32 >> p.log_lanes;
-  const bool live = e < p.D, turned = live && e < p.rot;
-  const int slot = blockIdx.y, kind = slot >= p.q_slots;
-  const int h0 = (kind ? p.q_heads + (slot - p.q_slots) * together * p.passes : slot * together * p.passes) + sub;
-  const int h1 = kind ? p.heads : p.q_heads;
-  const float inv_d = 1.0f / (float)p.D;
-  const int half = p.rot >> 1;
-  int src[V / 4];
-#pragma unroll
-  for (int q = 0; q < V / 4; q++) {
-    const int e0 = e + 4 * q;
-    const int pe = e0 < half ? e0 + half : e0 - half;
-    src[q] = live && e0 < p.rot ? (lane - g) + pe / V : lane;
-  }
-  const bool odd = (half & 4) != 0;
-  pdl_begin();
+// OP 0: rotation, 1: norm and rotation, 2: backward of 1.  A warp takes the heads of a row in passes of `together`; in the
+// backward queries and keys are taken by different blocks (grid y), each with one set of sums in registers.
+// PASSES, and BLOCKS of 256 threads on an SM (80 or 128 registers), were tried together; 16384 rows x 24 heads x 64 and 8144 x 20
+// x 128, us: rotation 3 x 4 18.8 and 16.2, 3 x 3 19.7 and 18.5, 2 x 3 21.6 and 18.5; norm 2 x 3 25.6 and 23.9, 3 x 3 32 and
+// 27, 3 x 2 27 and 28; backward 3 x 2 44 and 43, 2 x 3 54 and 40.  Asking for a row ahead gained nothing at any of them.
+template <int OP> struct Shape {
+  static constexpr int PASSES = OP == 1 ? 2 : 3, BLOCKS = OP == 0 ? 4 : OP == 1 ? 3 : 2;
+};
 
-  uint64_t turns[NT];
-#pragma unroll
-  for (int j = 0; j < NT; j += 2) {
-    int i;
-    bool act;
-    if (INTER) {
-      i = e / 2 + j;
-      act = turned;
-    } else {
-      const int e0 = e + (j & ~3);
-      act = live && e0 < p.rot;
-      i = (e0 < half ? e0 : e0 - half) + (j & 3);
-    }
-    ulonglong2 t = make_ulonglong2(0, 0);
-    if (act) t = *reinterpret_cast<const ulonglong2*>(p.turns + i);
-    turns[j] = t.x;
-    turns[j + 1] = t.y;
-  }
-  float gain[V], bias[V], dgain[V], dbias[V];
+template <typename T, bool INTER, int OP>
+__global__ void __launch_bounds__(32 * RO_WARPS, Shape<OP>::BLOCKS)
+rotary_kernel(const RotaryParams p) {
+  constexpr bool kExact = sizeof(T) == 4;
+  constexpr int PASSES = Shape<OP>::PASSES;
+  typedef Piece<T> Pc;
+  typedef typename Pc::Raw Raw;
+  __shared__ __align__(16) uint64_t turns[64];
+  __shared__ __align__(16) float gains[OP >= 1 ? 2 : 1][128], biases[OP == 1 ? 2 : 1][128];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lanes = 1 << p.log_lanes, o = (lane & (lanes - 1)) * W, half = p.rot >> 1;
+  const int sub = lane >> p.log_lanes, together = 32 >> p.log_lanes;
+  const bool live = o < p.D / 2;
+  const int ea = INTER ? 2 * o : o < half ? o : half + o;                        // half + o = rot + (o - half)
+  const int eb = INTER ? 2 * o + W : o < half ? half + o : p.D / 2 + o;          // rot + (D - rot) / 2 + (o - half)
+  const bool turn_a = live && (INTER ? ea < p.rot : o < half), turn_b = live && (INTER ? eb < p.rot : o < half);
+  const int slot = blockIdx.y, kind = OP == 2 && slot >= p.q_slots;
+  const int h0 = (kind ? p.q_heads + (slot - p.q_slots) * together * p.passes : slot * together * p.passes) + sub;
+  const int h1 = OP < 2 || kind ? p.heads : p.q_heads;
+  const float inv_d = 1.0f / (float)p.D;
+  pdl_begin();
+  for (int i = threadIdx.x; i < 64; i += 32 * RO_WARPS) turns[i] = i < half ? p.turns[i] : 0;
   if (OP >= 1) {
-#pragma unroll
-    for (int j = 0; j < V; j++) {
-      gain[j] = live ? p.gain[kind * p.D + e + j] : 0.f;
-      bias[j] = OP == 1 && live && p.bias ? p.bias[kind * p.D + e + j] : 0.f;
-      dgain[j] = dbias[j] = 0.f;
+    for (int i = threadIdx.x; i < 2 * p.D; i += 32 * RO_WARPS) {
+      const int k = i >= p.D;
+      gains[k][i - k * p.D] = p.gain[i];
+      if (OP == 1) biases[k][i - k * p.D] = p.bias ? p.bias[i] : 0.f;
     }
   }
+  __syncthreads();
+  float dga[W], dgb[W], dba[W], dbb[W];
+#pragma unroll
+  for (int j = 0; j < W; j++) dga[j] = dgb[j] = dba[j] = dbb[j] = 0.f;
+
+  const T* x0 = (const T*)p.x + h0 * p.x_head;
+  const T* d0 = (const T*)p.dy + h0 * p.dy_head;
+  T* out0 = OP == 2 ? (T*)p.dx + h0 * p.dx_head : (T*)p.y + h0 * p.y_head;
+  const int64_t x_step = together * p.x_head, d_step = together * p.dy_head;
+  const int64_t out_row = OP == 2 ? p.dx_row : p.y_row, out_step = together * (OP == 2 ? p.dx_head : p.y_head);
+  bool here[PASSES];
+#pragma unroll
+  for (int k = 0; k < PASSES; k++) here[k] = k < p.passes && live && h0 + k * together < h1;
 
   for (int row = (int)blockIdx.x * RO_WARPS + warp; row < p.rows; row += (int)gridDim.x * RO_WARPS) {
-    typename VecT<T>::Raw rx[RO_PASSES], rd[RO_PASSES];
+    Raw xa[PASSES], xb[PASSES], da[PASSES], db[PASSES];
     const int pos = p.positions ? p.positions[row] : row % p.seq;
 #pragma unroll
-    for (int k = 0; k < RO_PASSES; k++) {
-      const int h = h0 + k * together;
-      if (k < p.passes && live && h < h1) {
-        rx[k] = VecT<T>::load_raw((const T*)p.x + row * p.x_row + h * p.x_head + e);
-        if (OP == 2) rd[k] = VecT<T>::load_raw((const T*)p.dy + row * p.dy_row + h * p.dy_head + e);
+    for (int k = 0; k < PASSES; k++) {
+      xa[k] = xb[k] = da[k] = db[k] = Raw();
+      if (here[k]) {
+        const T* x = x0 + row * p.x_row + k * x_step;
+        xa[k] = *reinterpret_cast<const Raw*>(x + ea);
+        xb[k] = *reinterpret_cast<const Raw*>(x + eb);
+        if (OP == 2) {
+          const T* d = d0 + row * p.dy_row + k * d_step;
+          da[k] = *reinterpret_cast<const Raw*>(d + ea);
+          db[k] = *reinterpret_cast<const Raw*>(d + eb);
+        }
       }
     }
-    float c[V], s[V];
+    float c[W], s[W];
 #pragma unroll
-    for (int j = 0; j < NT; j++) {
-      float sn, cs;
-      turn_of(pos, turns[j], kExact, sn, cs);
-      sn *= p.sign * p.magnitude;
-      cs *= p.magnitude;
-      if (INTER) {
-        c[2 * j] = turned ? cs : 1.f;
-        c[2 * j + 1] = c[2 * j];
-        s[2 * j + 1] = turned ? sn : 0.f;
-        s[2 * j] = -s[2 * j + 1];
-      } else {
-        const int e0 = e + (j & ~3);
-        const bool act = e0 < p.rot;
-        c[j] = act ? cs : 1.f;
-        s[j] = !act ? 0.f : e0 < half ? -sn : sn;
-      }
+    for (int j = 0; j < W; j++) {
+      turn_of(pos, turns[(o + j) & 63], kExact, s[j], c[j]);
+      s[j] *= p.sign * p.magnitude;
+      c[j] *= p.magnitude;
     }
+    float mean[PASSES], r[PASSES];
+    if (OP >= 1) {
 #pragma unroll
-    for (int k = 0; k < RO_PASSES; k++) {
-      if (k >= p.passes) break;
-      const int h = h0 + k * together;
-      const bool here = live && h < h1;
-      float v[V];
+      for (int k = 0; k < PASSES; k++) mean[k] = r[k] = 0.f;
+      if (p.center) {
 #pragma unroll
-      for (int j = 0; j < V; j++) v[j] = 0.f;
-      if (here) VecT<T>::unpack(rx[k], v);
-      if (OP >= 1) {
-        float mean = 0.f, sum = 0.f;
-        if (p.center) {
+        for (int k = 0; k < PASSES; k++) {
+          float a[W], b[W];
+          Pc::unpack(xa[k], a);
+          Pc::unpack(xb[k], b);
 #pragma unroll
-          for (int j = 0; j < V; j++) sum += v[j];
-          mean = lanes_sum(sum, p.log_lanes) * inv_d;
+          for (int j = 0; j < W; j++) mean[k] += a[j] + b[j];
         }
-        sum = 0.f;
+        lanes_sum(mean, lanes);
 #pragma unroll
-        for (int j = 0; j < V; j++) {
-          if (here) v[j] -= mean;
-          sum = fmaf(v[j], v[j], sum);
+        for (int k = 0; k < PASSES; k++) mean[k] = here[k] ? mean[k] * inv_d : 0.f;  // an idle lane's zeros stay zeros
+      }
+#pragma unroll
+      for (int k = 0; k < PASSES; k++) {
+        float a[W], b[W];
+        Pc::unpack(xa[k], a);
+        Pc::unpack(xb[k], b);
+#pragma unroll
+        for (int j = 0; j < W; j++) {
+          a[j] -= mean[k];
+          b[j] -= mean[k];
+          r[k] = fmaf(a[j], a[j], r[k]);
+          r[k] = fmaf(b[j], b[j], r[k]);
         }
-        const float r = 1.0f / sqrtf(fmaf(lanes_sum(sum, p.log_lanes), inv_d, p.eps));
+      }
+      lanes_sum(r, lanes);
 #pragma unroll
-        for (int j = 0; j < V; j++) v[j] *= r;  // xh
+      for (int k = 0; k < PASSES; k++) r[k] = rsqrtf(fmaf(r[k], inv_d, p.eps));
+    }
+    if (OP == 2) {
+      float a[PASSES][W], b[PASSES][W], u[PASSES][W], w[PASSES][W], m1[PASSES], m2[PASSES];
+      float ga[W], gb[W];
+#pragma unroll
+      for (int j = 0; j < W; j++) {
+        ga[j] = live ? gains[kind][ea + j] : 0.f;
+        gb[j] = live ? gains[kind][eb + j] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < PASSES; k++) {
+        Pc::unpack(xa[k], a[k]);
+        Pc::unpack(xb[k], b[k]);
+        Pc::unpack(da[k], u[k]);
+        Pc::unpack(db[k], w[k]);
+        rotate<INTER>(u[k], w[k], c, s, turn_a, turn_b);
+        m1[k] = m2[k] = 0.f;
+#pragma unroll
+        for (int j = 0; j < W; j++) {
+          a[k][j] = (a[k][j] - mean[k]) * r[k];  // xh
+          b[k][j] = (b[k][j] - mean[k]) * r[k];
+          dga[j] = fmaf(u[k][j], a[k][j], dga[j]);
+          dgb[j] = fmaf(w[k][j], b[k][j], dgb[j]);
+          dba[j] += u[k][j];
+          dbb[j] += w[k][j];
+          u[k][j] *= ga[j];
+          w[k][j] *= gb[j];
+          m1[k] = fmaf(u[k][j], a[k][j], m1[k]);
+          m1[k] = fmaf(w[k][j], b[k][j], m1[k]);
+          m2[k] += u[k][j] + w[k][j];
+        }
+      }
+      lanes_sum(m1, lanes);
+      if (p.center) lanes_sum(m2, lanes);
+#pragma unroll
+      for (int k = 0; k < PASSES; k++) {
+        m1[k] *= inv_d;
+        m2[k] = p.center ? m2[k] * inv_d : 0.f;
+#pragma unroll
+        for (int j = 0; j < W; j++) {
+          a[k][j] = r[k] * (u[k][j] - m2[k] - a[k][j] * m1[k]);
+          b[k][j] = r[k] * (w[k][j] - m2[k] - b[k][j] * m1[k]);
+        }
+        if (here[k]) {
+          T* out = out0 + row * out_row + k * out_step;
+          Pc::store(out + ea, a[k]);
+          Pc::store(out + eb, b[k]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < PASSES; k++) {
+        if (!here[k]) continue;
+        float a[W], b[W];
+        Pc::unpack(xa[k], a);
+        Pc::unpack(xb[k], b);
         if (OP == 1) {
-#pragma unroll
-          for (int j = 0; j < V; j++) v[j] = fmaf(v[j], gain[j], bias[j]);
-        } else {
-          float d[V];
-#pragma unroll
-          for (int j = 0; j < V; j++) d[j] = 0.f;
-          if (here) VecT<T>::unpack(rd[k], d);
-          rotate<V, INTER>(d, c, s, src, odd);
-          float m1 = 0.f, m2 = 0.f;
-#pragma unroll
-          for (int j = 0; j < V; j++) {
-            dgain[j] = fmaf(d[j], v[j], dgain[j]);
-            dbias[j] += d[j];
-            d[j] *= gain[j];
-            m1 = fmaf(d[j], v[j], m1);
-            m2 += d[j];
+          const int kd = h0 + k * together >= p.q_heads;
+          const float4 ga = *reinterpret_cast<const float4*>(&gains[kd][ea]), gb = *reinterpret_cast<const float4*>(&gains[kd][eb]);
+          float4 ba = make_float4(0.f, 0.f, 0.f, 0.f), bb = ba;
+          if (p.bias) {
+            ba = *reinterpret_cast<const float4*>(&biases[kd][ea]);
+            bb = *reinterpret_cast<const float4*>(&biases[kd][eb]);
           }
-          m1 = lanes_sum(m1, p.log_lanes) * inv_d;
-          m2 = p.center ? lanes_sum(m2, p.log_lanes) * inv_d : 0.f;
+          const float g4[2][W] = {{ga.x, ga.y, ga.z, ga.w}, {gb.x, gb.y, gb.z, gb.w}};
+          const float b4[2][W] = {{ba.x, ba.y, ba.z, ba.w}, {bb.x, bb.y, bb.z, bb.w}};
 #pragma unroll
-          for (int j = 0; j < V; j++) v[j] = r * (d[j] - m2 - v[j] * m1);
-          if (here) VecT<T>::store((T*)p.dx + row * p.dx_row + h * p.dx_head + e, v);
+          for (int j = 0; j < W; j++) {
+            a[j] = fmaf((a[j] - mean[k]) * r[k], g4[0][j], b4[0][j]);
+            b[j] = fmaf((b[j] - mean[k]) * r[k], g4[1][j], b4[1][j]);
+          }
         }
-      }
-      if (OP <= 1) {
-        rotate<V, INTER>(v, c, s, src, odd);
-        if (here) VecT<T>::store((T*)p.y + row * p.y_row + h * p.y_head + e, v);
+        rotate<INTER>(a, b, c, s, turn_a, turn_b);
+        T* out = out0 + row * out_row + k * out_step;
+        Pc::store(out + ea, a);
+        Pc::store(out + eb, b);
       }
     }
   }
 
   if (OP == 2) {  // the block's sums, warps and groups in order
-    __shared__ float part[RO_WARPS][2][32 * V];
+    __shared__ float part[RO_WARPS][2][64 * W];  // together * D <= 64 W
+    if (live) {
 #pragma unroll
-    for (int j = 0; j < V; j++) {
-      part[warp][0][lane * V + j] = dgain[j];
-      part[warp][1][lane * V + j] = dbias[j];
+      for (int j = 0; j < W; j++) {
+        part[warp][0][sub * p.D + ea + j] = dga[j];
+        part[warp][0][sub * p.D + eb + j] = dgb[j];
+        part[warp][1][sub * p.D + ea + j] = dba[j];
+        part[warp][1][sub * p.D + eb + j] = dbb[j];
+      }
     }
     __syncthreads();
     float* out = p.partial + (int64_t)(blockIdx.y * gridDim.x + blockIdx.x) * 2 * p.D;
@@ -228,13 +322,13 @@ rotary_kernel(const RotaryParams p) {
       const int which = i >= p.D, col = i - which * p.D;
       float sum = 0.f;
       for (int w = 0; w < RO_WARPS; w++)
-        for (int t = 0; t < together; t++) sum += part[w][which][t * lanes * V + col];
+        for (int t = 0; t < together; t++) sum += part[w][which][t * p.D + col];
       out[i] = sum;
     }
   }
 }
 
-// Sums of the blocks' sums, in order: 32 columns a block, 32 threads each, added in double at the end.
+// Sums of the blocks' sums, in order: 32 columns a block, 32 threads each, added in double.
 __global__ void __launch_bounds__(1024) rotary_sum_kernel(const float* partial, int D, int q_blocks, int blocks, float* dgain,
                                                           float* dbias) {
   __shared__ double part[32][33];
@@ -257,17 +351,18 @@ __global__ void __launch_bounds__(1024) rotary_sum_kernel(const float* partial, 
 
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-// The launch of all three forms.  passes: a warp takes up to four groups of heads, fewer where the launch would have too
-// few warps to fill the device (latency counts there, and the angles cost little).
+// passes: a warp takes up to PASSES groups of heads, fewer where the launch would have too few warps to fill the
+// device (latency counts there, and the angles cost little).
 struct RotaryLaunch { dim3 grid; int q_blocks; };
-RotaryLaunch plan_rotary(RotaryParams& p, int vec, int blocks_per_sm, int sms) {
+RotaryLaunch plan_rotary(RotaryParams& p, int most_passes, int blocks_per_sm, int sms, bool by_kind) {
   p.log_lanes = 0;
-  while ((vec << p.log_lanes) < p.D) p.log_lanes++;
-  const int together = 32 >> p.log_lanes, k_heads = p.heads - p.q_heads;
+  while ((2 * W << p.log_lanes) < p.D) p.log_lanes++;
+  const int together = 32 >> p.log_lanes;
+  const int first = by_kind ? p.q_heads : p.heads, second = p.heads - first;
   int slots = 0;
-  for (p.passes = RO_PASSES; p.passes >= 1; p.passes--) {
-    p.q_slots = ceil_div(p.q_heads, together * p.passes);
-    slots = p.q_slots + ceil_div(k_heads, together * p.passes);
+  for (p.passes = most_passes; p.passes >= 1; p.passes--) {
+    p.q_slots = ceil_div(first, together * p.passes);
+    slots = p.q_slots + ceil_div(second, together * p.passes);
     if (p.passes == 1 || (int64_t)p.rows * slots >= (int64_t)sms * RO_WARPS * blocks_per_sm) break;
   }
   const int most = sms * blocks_per_sm > RO_MAX_BLOCKS ? RO_MAX_BLOCKS : sms * blocks_per_sm;
@@ -282,8 +377,7 @@ RotaryLaunch plan_rotary(RotaryParams& p, int vec, int blocks_per_sm, int sms) {
 
 template <int OP>
 RotaryLaunch run_rotary(const mslt_rope_desc& d, RotaryParams& p, int sms, cudaStream_t st) {
-  // blocks of 256 threads that an SM holds at the kernels' registers
-  const RotaryLaunch l = plan_rotary(p, d.dtype == 1 ? 8 : 4, OP == 2 ? 2 : 3, sms);
+  const RotaryLaunch l = plan_rotary(p, Shape<OP>::PASSES, Shape<OP>::BLOCKS, sms, OP == 2);
   if (d.dtype == 1) {
     if (d.interleaved) launch_pdl(rotary_kernel<bf16, true, OP>, l.grid, 32 * RO_WARPS, 0, st, p);
     else launch_pdl(rotary_kernel<bf16, false, OP>, l.grid, 32 * RO_WARPS, 0, st, p);
