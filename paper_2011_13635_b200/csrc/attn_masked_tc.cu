@@ -8,10 +8,13 @@
 // P and dS are the A operand of the second product and never leave tensor memory: they are written over the scores they
 // come from.  dQ and dK/dV are two launches that form S and dP twice (7 products in the place of 5): in return no sum
 // crosses blocks, so every run gives the same bits and nothing is added by atomics.
-//   warp 0: TMA producer; warp 1: one thread issues the products; warps 2-5: softmax
-// Two blocks share an SM where 256 columns of tensor memory and half of the shared memory do (all but the backward of
-// heads wider than 64): while one waits for its products, the other has the exponential unit, which bounds heads of 64 (a
-// 128 x 128 tile takes 1024 cycles of exponentials, its products 512 in the forward).
+//   warp 0: TMA producer; warp 1: one thread issues the products; the others: softmax, a thread a row (forward) or half a
+//   row's columns (backward, where the rows' sums are known)
+// What bounds it: the exponential unit takes 512 cycles for 128 x 64 scores, the forward's products 256 (heads of 64), and
+// around both lies a chain of waits and tensor-memory reads of some 1500 cycles a loop block.  So blocks are small and many
+// share an SM, one working while the others wait: heads of 64, four forward blocks (128 columns of tensor memory, 80
+// registers, scores read twice in the place of 64 registers) and two backward blocks of eight softmax warps.  Measured
+// with two forward blocks of double-buffered scores: a loop block took 1660 cycles of a block, 1120 of the SM.
 //
 // Which blocks a row tile visits is worked out once, at its start, from positions, length, prefix and the least and
 // greatest document of either side: left out, whole, or with pairs to test.  Documents may be in any order; where they
@@ -34,12 +37,13 @@ namespace {
 
 constexpr int AM_ROWS = 128;      // rows of a block
 constexpr int AM_COLS = 64;       // rows of a loop block
-constexpr int AM_THREADS = 192;
-constexpr int AM_SOFT = 4;        // softmax warps
+constexpr int AF_SOFT = 4, AF_THREADS = 64 + 32 * AF_SOFT;  // forward: softmax warps, threads
+constexpr int AB_SOFT = 8, AB_THREADS = 64 + 32 * AB_SOFT;  // backward
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // The running maximum of a row is followed only where it grows by more than 2^8: until then the probabilities stay
 // below 2^8, which costs bf16 nothing, and the accumulator in tensor memory need not be read and written.
 constexpr float AM_SLACK = 8.0f;
+
 
 struct View { bf16* p; long long batch, row, head; };
 struct TcParams {
@@ -63,15 +67,20 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
       : "memory");
 }
 __device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -103,7 +112,7 @@ __device__ __forceinline__ Seq sequence(const AttnMask& m, int b) {
 
 // Called by the whole block.  list[i] receives 2 * block + (pairs to test); returns their number.  Rows r0 .. r0 + 127 are
 // queries (and the blocks keys), or with kKeys the other way round.  red: 16 words of shared memory.
-template <bool kKeys>
+template <bool kKeys, int kWarps>
 __device__ __forceinline__ int list_blocks(const AttnMask& m, const Seq& s, int b, int r0, uint16_t* list, int* red) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int* docs = m.docs ? m.docs + (long long)b * m.S : nullptr;
@@ -134,17 +143,17 @@ __device__ __forceinline__ int list_blocks(const AttnMask& m, const Seq& s, int 
   };
   if (docs) {
     constexpr int kAhead = 4;  // blocks whose documents are asked for together
-    for (int base = first + warp; base < last; base += (AM_THREADS / 32) * kAhead) {
+    for (int base = first + warp; base < last; base += kWarps * kAhead) {
       int d0[kAhead], d1[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
-        const int c = (base + u * (AM_THREADS / 32)) * AM_COLS + lane;
+        const int c = (base + u * kWarps) * AM_COLS + lane;
         d0[u] = c < s.len ? docs[c] : 0;
         d1[u] = c + 32 < s.len ? docs[c + 32] : 0;
       }
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
-        const int blk = base + u * (AM_THREADS / 32), c = blk * AM_COLS + lane;
+        const int blk = base + u * kWarps, c = blk * AM_COLS + lane;
         int mn = min(c < s.len ? d0[u] : 0x7fffffff, c + 32 < s.len ? d1[u] : 0x7fffffff);
         int mx = max(c < s.len ? d0[u] : (int)0x80000000, c + 32 < s.len ? d1[u] : (int)0x80000000);
         mn = __reduce_min_sync(0xffffffffu, mn);
@@ -173,48 +182,121 @@ __device__ __forceinline__ int list_blocks(const AttnMask& m, const Seq& s, int 
   return red[8];
 }
 
-// Which of the 64 loop rows from c0 on row r counts a pair with.  docs: the 64 loop rows' documents in shared memory.
+// Which of the 32 loop rows from c0 on row r counts a pair with; the whole warp.  The loop rows' documents lie one a lane;
+// the warp's own rows seldom hold more than two or three, and each of those takes one ballot for all rows that have it.
 template <bool kKeys>
-__device__ __forceinline__ uint64_t visible(const Seq& s, int r, int c0, bool has_docs, int doc, const int* docs) {
+__device__ __forceinline__ uint32_t visible(const Seq& s, int r, int c0, const int* docs, int doc) {
   const int end = (kKeys ? s.len : min(s.len, max(r + 1, s.prefix))) - c0;
   const int begin = (kKeys && r >= s.prefix ? r : 0) - c0;
-  uint64_t w = end >= 64 ? ~0ull : end <= 0 ? 0ull : (1ull << end) - 1;
-  if (begin > 0) w = begin >= 64 ? 0ull : w & ~((1ull << begin) - 1);
-  if (has_docs) {
-    uint32_t a = 0, b = 0;
-#pragma unroll
-    for (int c = 0; c < 32; c += 4) {
-      const int4 x = *reinterpret_cast<const int4*>(docs + c), y = *reinterpret_cast<const int4*>(docs + 32 + c);
-      a |= (x.x == doc ? 1u << c : 0) | (x.y == doc ? 2u << c : 0) | (x.z == doc ? 4u << c : 0) | (x.w == doc ? 8u << c : 0);
-      b |= (y.x == doc ? 1u << c : 0) | (y.y == doc ? 2u << c : 0) | (y.z == doc ? 4u << c : 0) | (y.w == doc ? 8u << c : 0);
+  uint32_t w = end >= 32 ? 0xffffffffu : end <= 0 ? 0u : (1u << end) - 1;
+  if (begin > 0) w = begin >= 32 ? 0u : w & ~((1u << begin) - 1);
+  if (docs) {
+    const int c = c0 + (int)(threadIdx.x & 31);
+    const int other = c < s.len ? docs[c] : 0;
+    uint32_t same = 0, todo = 0xffffffffu;
+    while (todo) {
+      const int v = __shfl_sync(0xffffffffu, doc, __ffs(todo) - 1);
+      const uint32_t has = __ballot_sync(0xffffffffu, other == v);
+      if (doc == v) same = has;
+      todo &= ~__ballot_sync(0xffffffffu, doc == v);
     }
-    w &= (uint64_t)b << 32 | a;
+    w &= same;
   }
   return w;
 }
 
 // ---- scores ---------------------------------------------------------------------------------------------
 
-// How a score becomes an exponent of two: 0: s scale log2(e), scale > 0; 1: a bias by distance, or a scale <= 0; 2: capped
-// (and perhaps biased).
-struct Form { float sl2, z_by, cap2, slope2; };
+// How a dot product becomes an exponent of two: 0: s scale log2(e), scale > 0; 1: a bias by distance, or a scale <= 0; 2:
+// capped (and perhaps biased).
+//
+// The cap, cap tanh(z / cap).  The hardware's tanh has an error of 2^-11 of the value: a probability off by 2 % at a score of
+// 50.  Where |z| <= 3/4 cap throughout a warp's piece, tanh(u) is u times a polynomial of degree 5 in u^2 (least greatest error
+// on u^2 <= 9/16, 2.7e-8 of the value), on the multiply-add pipe and with all constants folded in; beyond,
+// 1 - 2 / (1 + e^(2u)), two special functions on top of the exponential's one, absolute error 2e-7.
+struct Form { float sl2, slope2, cap2, inv_cap2, z_by, small, b[6]; };
+template <int kForm>
 __device__ __forceinline__ Form form_of(const AttnMask& m, int h) {
   Form f;
   f.sl2 = m.scale * LOG2E;
-  f.z_by = m.cap > 0.f ? m.scale / m.cap * (2.f * LOG2E) : 0.f;  // 2^(s z_by) = e^(2 z / cap)
-  f.cap2 = m.cap * LOG2E;
-  f.slope2 = m.slopes ? m.slopes[h] * LOG2E : 0.f;
+  f.slope2 = kForm >= 1 && m.slopes ? m.slopes[h] * LOG2E : 0.f;
+  if (kForm == 2) {
+    constexpr float kT[6] = {0.999999973f, -0.333329788f, 0.133256886f, -0.0533584462f, 0.0196113117f, -0.00473641511f};
+    const float k = m.scale / m.cap;
+    f.cap2 = m.cap * LOG2E;
+    f.inv_cap2 = 1.f / f.cap2;
+    f.z_by = k * (2.f * LOG2E);  // 2^(s z_by) = e^(2 z / cap)
+    f.small = 0.75f / fabsf(k);
+    float by = f.cap2 * k;
+#pragma unroll
+    for (int i = 0; i < 6; i++) {
+      f.b[i] = kT[i] * by;
+      by *= k * k;
+    }
+  }
   return f;
 }
-// dist: distance of the pair.  bend: derivative of the cap.  tanh u = 1 - 2 / (1 + e^(2u)): two special functions and an
-// absolute error of 2e-7, where the hardware's tanh has 2^-11 of the value (a probability off by 2 % at a score of 50).
+// A warp's piece of 32 columns: what is the same for all of it.  side: 0 the distance of pairs needs its absolute value, 1
+// all columns lie before all rows of the warp, -1 behind; then the bias is linear in the column.
+struct Piece { float off; int side; bool small; };
 template <int kForm>
-__device__ __forceinline__ float exponent(const Form& f, float s, float dist, float* bend) {
-  if (kForm == 0) return s * f.sl2;
-  if (kForm == 1) return fmaf(s, f.sl2, -f.slope2 * dist);
-  const float t = fmaf(-2.f, rcp(1.f + ex2(s * f.z_by)), 1.f);
-  *bend = fmaf(-t, t, 1.f);
-  return fmaf(f.cap2, t, -f.slope2 * dist);
+__device__ __forceinline__ Piece piece_of(const Form& f, int r, int c0, const uint32_t (&s)[32]) {
+  Piece p;
+  p.off = (float)(c0 - r);
+  const int r_first = r - (int)(threadIdx.x & 31);
+  p.side = c0 + 31 <= r_first ? 1 : c0 >= r_first + 31 ? -1 : 0;
+  p.small = true;
+  if (kForm == 2) {
+    float m = 0.f;
+#pragma unroll
+    for (int c = 0; c < 32; c += 2) m = fmaxf(m, fmaxf(fabsf(__uint_as_float(s[c])), fabsf(__uint_as_float(s[c + 1]))));
+    p.small = __all_sync(0xffffffffu, m <= f.small);
+  }
+  return p;
+}
+// What a piece needs is decided once for all of it: BIAS 0 none, 1 linear in the column, 2 by absolute value; CAP 0 none, 1 the
+// polynomial, 2 special functions; TEST: pairs to test.  (Decided pair by pair, the instructions of the other ways are
+// issued too, without effect: 710 in the place of 400 for the 64 columns of a row, twice the time with a bias.)
+template <int kBias, int kCap, bool kTest> struct Way { static constexpr int BIAS = kBias, CAP = kCap; static constexpr bool TEST = kTest; };
+template <int kForm, typename F>
+__device__ __forceinline__ void choose_way(const Form& f, const Piece& p, bool test, F&& body) {
+  if (kForm == 0) {
+    if (test) body(Way<0, 0, true>()); else body(Way<0, 0, false>());
+  } else if (kForm == 1) {
+    if (test) body(Way<2, 0, true>());
+    else if (p.side) body(Way<1, 0, false>());
+    else body(Way<2, 0, false>());
+  } else if (f.slope2 == 0.f) {
+    if (p.small) { if (test) body(Way<0, 1, true>()); else body(Way<0, 1, false>()); }
+    else body(Way<0, 2, true>());
+  } else {
+    if (p.small && !test) body(Way<2, 1, false>());
+    else body(Way<2, 2, true>());
+  }
+}
+// exponents of columns c and c + 1 of the piece, plus nb; bend: derivative of the cap
+template <typename Wy, bool kBend>
+__device__ __forceinline__ float2 exponents(const Form& f, const Piece& p, float2 s, int c, float2 nb, float2* bend) {
+  float2 t = nb;
+  if (Wy::BIAS == 1) {
+    const float by = p.side > 0 ? f.slope2 : -f.slope2, at = by * p.off;
+    t = __fadd2_rn(nb, make_float2(fmaf(by, (float)c, at), fmaf(by, (float)(c + 1), at)));
+  }
+  if (Wy::BIAS == 2) t = make_float2(fmaf(-f.slope2, fabsf(p.off + (float)c), nb.x), fmaf(-f.slope2, fabsf(p.off + (float)(c + 1)), nb.y));
+  if (Wy::CAP == 0) return __ffma2_rn(s, splat2(f.sl2), t);
+  if (Wy::CAP == 1) {
+    const float2 y = __fmul2_rn(s, s);
+    float2 q = splat2(f.b[5]);
+#pragma unroll
+    for (int i = 4; i >= 0; i--) q = __ffma2_rn(q, y, splat2(f.b[i]));
+    if (!kBend) return __ffma2_rn(s, q, t);
+    const float2 v = __fmul2_rn(s, q), th = __fmul2_rn(v, splat2(f.inv_cap2));
+    *bend = __ffma2_rn(make_float2(-th.x, -th.y), th, splat2(1.f));
+    return __fadd2_rn(v, t);
+  }
+  const float2 th = make_float2(fmaf(-2.f, rcp(1.f + ex2(s.x * f.z_by)), 1.f), fmaf(-2.f, rcp(1.f + ex2(s.y * f.z_by)), 1.f));
+  if (kBend) *bend = __ffma2_rn(make_float2(-th.x, -th.y), th, splat2(1.f));
+  return __ffma2_rn(splat2(f.cap2), th, t);
 }
 
 // ---- pieces of the roles ----------------------------------------------------------------------------------
@@ -236,12 +318,13 @@ __device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t a_kb
       tc_mma(d, ad, bd, idesc, kb + k > 0 ? 1u : 0u);
     }
 }
-// D (+)= A B, A 64 wide in tensor memory, B 64 rows (the contraction) of DP contiguous elements
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+// D (+)= A B, A 64 wide in tensor memory (its second half `a_half` columns behind the first), B 64 rows (the
+// contraction) of DP contiguous elements
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t a_half, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   const uint32_t hi = (uint32_t)(make_smem_desc(0, 16) >> 32), lo = (uint32_t)make_smem_desc(0, 8192);
 #pragma unroll
   for (int k = 0; k < 4; k++)
-    tc_mma_ts(d, a + k * 8, ((uint64_t)hi << 32) | (lo + addr16(b) + k * 128), idesc, accumulate | (k > 0));
+    tc_mma_ts(d, a + (k >> 1) * a_half + (k & 1) * 8, ((uint64_t)hi << 32) | (lo + addr16(b) + k * 128), idesc, accumulate | (k > 0));
 }
 
 template <int DP>
@@ -262,48 +345,43 @@ __device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
   while (!mbar_try_wait(smem_u32(bar), parity) && now_cycles() - t0 < 200000000ll) {}
 }
 
-// Rows `from` .. 63 of a loop block's tiles become zero; the whole softmax group, thread t of 128.
-template <int DP>
+// Rows `from` .. 63 of a loop block's tiles become zero; the whole softmax group, thread t of kThreads.
+template <int DP, int kThreads>
 __device__ __forceinline__ void clear_rows(uint8_t* tile, int from, int t) {
 #pragma unroll
   for (int kb = 0; kb < DP / 64; kb++)
-    for (int v = from * 8 + t; v < AM_COLS * 8; v += AM_SOFT * 32)
+    for (int v = from * 8 + t; v < AM_COLS * 8; v += kThreads)
       reinterpret_cast<uint4*>(tile + kb * 8192)[v] = make_uint4(0, 0, 0, 0);
 }
 
-// 32 columns of a row, scaled, to bf16; optionally what the rounding took off
-__device__ __forceinline__ void store32(bf16* dst, bf16* rest, const uint32_t (&r)[32], float f, int cols) {
-#pragma unroll
-  for (int c = 0; c < 32; c += 8) {
-    if (c >= cols) break;
-    uint4 hi, lo;
-    uint32_t *h = reinterpret_cast<uint32_t*>(&hi), *l = reinterpret_cast<uint32_t*>(&lo);
-#pragma unroll
-    for (int e = 0; e < 4; e++) {
-      const float x = __uint_as_float(r[c + 2 * e]) * f, y = __uint_as_float(r[c + 2 * e + 1]) * f;
-      h[e] = pack2(x, y);
-      const float2 b = bf162_to_f2(h[e]);
-      l[e] = pack2(x - b.x, y - b.y);
-    }
-    *reinterpret_cast<uint4*>(dst + c) = hi;
-    if (rest) *reinterpret_cast<uint4*>(rest + c) = lo;
-  }
-}
-// A row of an accumulator (DP columns from taddr on) to memory; f = 0 stores zeros whatever the accumulator holds.
-template <int DP>
-__device__ __forceinline__ void store_row(uint32_t taddr, bf16* dst, bf16* rest, float f, bool zero, bool have, bool write, int D) {
-#pragma unroll
-  for (int c = 0; c < DP; c += 32) {
-    uint32_t r[32];
-    if (have) {
-      tc_ld32_issue(taddr + c, r);
-      tc_ld32_wait(r);
-    }
+// Columns [c0, c1) of a row of an accumulator, scaled, to bf16 in memory (from dst on), 16 at a time; optionally what the
+// rounding took off.  zero: zeros whatever the accumulator holds; have: there is one.
+__device__ __forceinline__ void store_row(uint32_t taddr, bf16* dst, bf16* rest, float f, bool zero, bool have, bool write, int c0, int c1,
+                                          int D) {
+#pragma unroll 2
+  for (int c = c0; c < c1; c += 16) {
+    uint32_t r[16];
+    if (have) tc_ld16(taddr + c, r);
     if (zero || !have) {
 #pragma unroll
-      for (int e = 0; e < 32; e++) r[e] = 0;
+      for (int e = 0; e < 16; e++) r[e] = 0;
     }
-    if (write) store32(dst + c, rest ? rest + c : nullptr, r, f, D - c);
+    if (!write) continue;
+#pragma unroll
+    for (int v = 0; v < 16; v += 8) {
+      if (c + v >= D) break;
+      uint4 hi, lo;
+      uint32_t *h = reinterpret_cast<uint32_t*>(&hi), *l = reinterpret_cast<uint32_t*>(&lo);
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const float x = __uint_as_float(r[v + 2 * e]) * f, y = __uint_as_float(r[v + 2 * e + 1]) * f;
+        h[e] = pack2(x, y);
+        const float2 b = bf162_to_f2(h[e]);
+        l[e] = pack2(x - b.x, y - b.y);
+      }
+      *reinterpret_cast<uint4*>(dst + c + v) = hi;
+      if (rest) *reinterpret_cast<uint4*>(rest + c + v) = lo;
+    }
   }
 }
 
@@ -330,18 +408,79 @@ __device__ __forceinline__ void settle(uint64_t* bar) {
 
 // ---- forward ----------------------------------------------------------------------------------------------
 
+// Heads of up to 64: 128 columns of tensor memory, four blocks an SM.  Wider ones need 256, so two blocks an SM have two
+// buffers of scores each.
 template <int DP> struct FwdShape {
-  static constexpr int STAGES = DP == 64 ? 4 : 2;
+  static constexpr int BLOCKS = DP == 64 ? 4 : 2, SB = DP == 64 ? 1 : 2, STAGES = 2;
+  static constexpr int COLS = DP == 64 ? 128 : 256, O_COL = SB * 64;
   static constexpr int Q_BYTES = AM_ROWS * DP * 2, KV_BYTES = AM_COLS * DP * 2;
   static constexpr int SMEM = Q_BYTES + 2 * STAGES * KV_BYTES;
 };
 
+// Probabilities of 32 columns: 2^(exponent - base), rounded to bf16; sums of the rounded and of the unrounded ones.  see: the
+// columns that count, all of them where there is nothing to test.
+template <int kForm>
+__device__ __forceinline__ void probabilities(const Form& f, const Piece& pc, const uint32_t (&s)[32], bool test, uint32_t see,
+                                              float base, uint32_t (&pk)[16], float2& sum, float2& exact) {
+  choose_way<kForm>(f, pc, test, [&](auto way) {
+    typedef decltype(way) Wy;
+#pragma unroll
+    for (int c = 0; c < 32; c += 2) {
+      float2 e = exponents<Wy, false>(f, pc, make_float2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), c, splat2(-base), nullptr);
+      if (Wy::TEST) {
+        e.x = see >> c & 1 ? e.x : -INFINITY;
+        e.y = see >> (c + 1) & 1 ? e.y : -INFINITY;
+      }
+      e.x = ex2(e.x);
+      e.y = ex2(e.y);
+      pk[c / 2] = pack2(e.x, e.y);
+      exact = __fadd2_rn(exact, e);
+      sum = __fadd2_rn(sum, bf162_to_f2(pk[c / 2]));
+    }
+  });
+}
+// Upper bound of the exponents of 32 columns that a row sees (-infinity: none), near enough to the largest to be the
+// reference of the row's exponents: without a bias it is the largest, with one it is above by at most 31 slopes, which
+// costs nothing but range while a slope is at most one power of two (a larger one is taken element by element).
+template <int kForm>
+__device__ __forceinline__ float largest(const Form& f, const Piece& pc, const uint32_t (&s)[32], bool test, uint32_t see) {
+  float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  if (kForm == 0 || (kForm == 1 && f.sl2 > 0.f && f.slope2 >= 0.f && f.slope2 <= 1.f)) {
+    if (test) {
+#pragma unroll
+      for (int c = 0; c < 32; c += 2) {
+        const float x = see >> c & 1 ? __uint_as_float(s[c]) : -INFINITY, y = see >> (c + 1) & 1 ? __uint_as_float(s[c + 1]) : -INFINITY;
+        m[c >> 1 & 3] = fmaxf(m[c >> 1 & 3], fmaxf(x, y));
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < 32; c += 2) m[c >> 1 & 3] = fmaxf(m[c >> 1 & 3], fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
+    }
+    const float big = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * f.sl2;
+    if (kForm == 0) return big;
+    return big - f.slope2 * (pc.off > 0.f ? pc.off : fmaxf(0.f, -31.f - pc.off));
+  }
+  choose_way<kForm>(f, pc, test, [&](auto way) {
+    typedef decltype(way) Wy;
+#pragma unroll
+    for (int c = 0; c < 32; c += 2) {
+      float2 e = exponents<Wy, false>(f, pc, make_float2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), c, splat2(0.f), nullptr);
+      if (Wy::TEST) {
+        e.x = see >> c & 1 ? e.x : -INFINITY;
+        e.y = see >> (c + 1) & 1 ? e.y : -INFINITY;
+      }
+      m[c >> 1 & 3] = fmaxf(m[c >> 1 & 3], fmaxf(e.x, e.y));
+    }
+  });
+  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+
 template <int DP, int kForm>
-__global__ void __launch_bounds__(AM_THREADS, 2)
+__global__ void __launch_bounds__(AF_THREADS, FwdShape<DP>::BLOCKS)
 masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
               const __grid_constant__ CUtensorMap tmV, const TcParams p) {
   typedef FwdShape<DP> Sh;
-  constexpr int NS = Sh::STAGES;
+  constexpr int NS = Sh::STAGES, SB = Sh::SB;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t* Ks = smem + Sh::Q_BYTES;
@@ -350,7 +489,6 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   __shared__ uint64_t qfull, kfull[NS], kempty[NS], vfull[NS], vempty[NS], sfull[2], pready[2], odone[2], oall;
   __shared__ uint32_t tmem_slot;
   __shared__ int red[16];
-  __shared__ __align__(16) int docs_of[AM_SOFT][AM_COLS];
   __shared__ __align__(8) int flag_mem[4];
   volatile int* abort_flag = flag_mem + 1;   // the limit, 8 bytes, follows
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -364,7 +502,7 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     }
     for (int i = 0; i < 2; i++) {
       mbar_init(smem_u32(&sfull[i]), 1);
-      mbar_init(smem_u32(&pready[i]), AM_SOFT);
+      mbar_init(smem_u32(&pready[i]), AF_SOFT);
       mbar_init(smem_u32(&odone[i]), 1);
     }
     mbar_init(smem_u32(&oall), 1);
@@ -377,7 +515,7 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     prefetch_map(&tmK);
     prefetch_map(&tmV);
   }
-  if (warp == 1) tmem_alloc<256>(&tmem_slot);
+  if (warp == 1) tmem_alloc<Sh::COLS>(&tmem_slot);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -388,8 +526,7 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   const int tile = p.m.causal ? p.tiles - 1 - idx : idx;  // causal: the tiles with the most keys start first
   const int hk = h / (p.heads / p.kv_heads), r0 = tile * AM_ROWS;
   const Seq s = sequence(p.m, b);
-  const int n = list_blocks<false>(p.m, s, b, r0, list, red);
-  constexpr uint32_t O_COL = 128;
+  const int n = list_blocks<false, AF_THREADS / 32>(p.m, s, b, r0, list, red);
 
   if (warp == 0 && n > 0 && !p.starve && elect_one()) {
     // ------------------------------- TMA producer -------------------------------
@@ -420,139 +557,114 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       const int st = j % NS;
       if (!mbar_wait(smem_u32(&kfull[st]), j / NS & 1, abort_flag, p.status)) return false;
       tc_fence_after();
-      product_ss<DP>(tmem + (j & 1) * 64, smem_u32(smem), 1024, smem_u32(Ks + st * Sh::KV_BYTES), 512, id_s);
+      product_ss<DP>(tmem + (j % SB) * 64, smem_u32(smem), 1024, smem_u32(Ks + st * Sh::KV_BYTES), 512, id_s);
       tc_commit(smem_u32(&sfull[j & 1]));
       tc_commit(smem_u32(&kempty[st]));
       return true;
     };
     bool ok = mbar_wait(smem_u32(&qfull), 0, abort_flag, p.status) && scores(0);
     for (int j = 0; j < n && ok; j++) {
-      if (j + 1 < n && !scores(j + 1)) { ok = false; break; }
+      if (SB == 2 && j + 1 < n && !scores(j + 1)) { ok = false; break; }
       const int st = j % NS;
       ok = mbar_wait(smem_u32(&vfull[st]), j / NS & 1, abort_flag, p.status) &&
            mbar_wait(smem_u32(&pready[j & 1]), j >> 1 & 1, abort_flag, p.status);
       if (!ok) break;
       tc_fence_after();
-      product_ts(tmem + O_COL, tmem + (j & 1) * 64, smem_u32(Vs + st * Sh::KV_BYTES), id_o, j > 0);
-      tc_commit(smem_u32(&odone[j & 1]));
+      product_ts(tmem + Sh::O_COL, tmem + (j % SB) * 64 + 32, 16, smem_u32(Vs + st * Sh::KV_BYTES), id_o, j > 0);
+      if (SB == 2) tc_commit(smem_u32(&odone[j & 1]));
       tc_commit(smem_u32(&vempty[st]));
+      // one buffer: the probabilities lie in it until the product with V, issued before, has read them
+      if (SB == 1 && j + 1 < n && !scores(j + 1)) { ok = false; break; }
     }
     if (ok) tc_commit(smem_u32(&oall));
     if (!ok || *abort_flag) settle(&oall);
   } else if (warp >= 2) {
     // ------------------------------- softmax: a thread owns a query -------------------------------
-    const int quarter = warp & 3, row = quarter * 32 + lane, r = r0 + row;
+    const int quarter = warp & 3, r = r0 + quarter * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16);
-    const Form f = form_of(p.m, h);
+    const Form f = form_of<kForm>(p.m, h);
     const int* docs = p.m.docs ? p.m.docs + (long long)b * p.m.S : nullptr;
     const int doc = docs && r < s.len ? docs[r] : 0;
-    float top = -INFINITY;               // reference of the row's exponents
-    float sum = 0.f, exact = 0.f;        // of the rounded probabilities, and of the unrounded ones
+    // Capped scores lie in [-cap, cap]: a cap of up to 44 (2^64) needs no reference, and the exponentials' range holds.
+    const bool fixed = kForm == 2 && f.cap2 <= 64.f && f.slope2 == 0.f;
+    float top = fixed ? 0.f : -INFINITY;                                  // reference of the row's exponents
+    float2 sum = make_float2(0.f, 0.f), exact = make_float2(0.f, 0.f);   // of the rounded probabilities, and of the unrounded ones
     bool ok = true;
     for (int j = 0; j < n; j++) {
       const int entry = list[j], c0 = (entry >> 1) * AM_COLS;
-      uint64_t see = ~0ull;
-      if (entry & 1) {
-        if (docs) {
-          __syncwarp();
-          docs_of[warp - 2][lane] = c0 + lane < s.len ? docs[c0 + lane] : 0;
-          docs_of[warp - 2][lane + 32] = c0 + lane + 32 < s.len ? docs[c0 + lane + 32] : 0;
-          __syncwarp();
-        }
-        see = visible<false>(s, r, c0, docs != nullptr, doc, docs_of[warp - 2]);
+      const bool test = entry & 1;
+      uint32_t see0 = ~0u, see1 = ~0u;
+      if (test) {
+        see0 = visible<false>(s, r, c0, docs, doc);
+        see1 = visible<false>(s, r, c0 + 32, docs, doc);
       }
       if (!mbar_wait(smem_u32(&sfull[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
       tc_fence_after();
-      uint32_t a0[32], a1[32];
-      tc_ld32_issue(trow + (j & 1) * 64, a0);
-      tc_ld32_issue(trow + (j & 1) * 64 + 32, a1);
-      tc_ld32_wait(a0);
-      tc_ld32_wait(a1);
-      float x[64];
-#pragma unroll
-      for (int c = 0; c < 32; c++) {
-        x[c] = __uint_as_float(a0[c]);
-        x[c + 32] = __uint_as_float(a1[c]);
+      const uint32_t tS = trow + (j % SB) * 64;
+      uint32_t a[32];
+      float big = -INFINITY;
+      if (!fixed) {
+        tc_ld32_issue(tS, a);
+        tc_ld32_wait(a);
+        big = largest<kForm>(f, piece_of<kForm>(f, r, c0, a), a, test, see0);
       }
-      if (kForm != 0) {
-        const float off = (float)(c0 - r);
+      tc_ld32_issue(tS + 32, a);
+      tc_ld32_wait(a);
+      Piece pc = piece_of<kForm>(f, r, c0 + 32, a);
+      if (!fixed) {
+        big = fmaxf(big, largest<kForm>(f, pc, a, test, see1));
+        const bool grow = big > top + AM_SLACK || (top == -INFINITY && big > top);
+        if (__any_sync(0xffffffffu, grow)) {
+          const float by = grow ? ex2(top - big) : 1.f;
+          if (grow) top = big;
+          sum = __fmul2_rn(sum, splat2(by));
+          exact = __fmul2_rn(exact, splat2(by));
+          if (j > 0) {
+            // The accumulator of the blocks so far.  One buffer of scores: they were issued behind the last product with V.
+            // Two: the scores at hand only say that the product before the last is complete, hence two barriers, so that
+            // neither can be a phase ahead.
+            if (SB == 2 && !mbar_wait(smem_u32(&odone[(j - 1) & 1]), (j - 1) >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 16) {
+              uint32_t o[16];
+              tc_ld16(trow + Sh::O_COL + c, o);
 #pragma unroll
-        for (int c = 0; c < 64; c++) {
-          float bend;
-          x[c] = exponent<kForm>(f, x[c], fabsf(off + (float)c), &bend);
-        }
-      }
-      if (entry & 1) {
-        const uint32_t w0 = (uint32_t)see, w1 = (uint32_t)(see >> 32);
-#pragma unroll
-        for (int c = 0; c < 32; c++) {
-          x[c] = w0 >> c & 1 ? x[c] : -INFINITY;
-          x[c + 32] = w1 >> c & 1 ? x[c + 32] : -INFINITY;
-        }
-      }
-      float mx[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-      for (int c = 4; c < 64; c += 8)
-#pragma unroll
-        for (int e = 0; e < 4; e++) mx[e] = c + 4 + e < 64 ? fmaxf(fmaxf(mx[e], x[c + e]), x[c + 4 + e]) : fmaxf(mx[e], x[c + e]);
-      float big = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-      if (kForm == 0) big *= f.sl2;
-      const bool grow = big > top + AM_SLACK || (top == -INFINITY && big > top);
-      if (__any_sync(0xffffffffu, grow)) {
-        const float by = grow ? ex2(top - big) : 1.f;
-        if (grow) top = big;
-        sum *= by;
-        exact *= by;
-        if (j > 0) {
-          // two barriers: the scores at hand say that the product before the last is complete, so neither can be a phase ahead
-          if (!mbar_wait(smem_u32(&odone[(j - 1) & 1]), (j - 1) >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
-          tc_fence_after();
-#pragma unroll
-          for (int c = 0; c < DP; c += 32) {
-            uint32_t o[32];
-            tc_ld32_issue(trow + O_COL + c, o);
-            tc_ld32_wait(o);
-#pragma unroll
-            for (int e = 0; e < 32; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-            tc_st32(trow + O_COL + c, o);
+              for (int e = 0; e < 16; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+              tc_st16(trow + Sh::O_COL + c, o);
+            }
           }
-          tc_st_wait();
         }
       }
       const float base = top == -INFINITY ? 0.f : top;
-      uint32_t pk[32];
-      float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)}, part_r[2] = {part[0], part[0]};
-#pragma unroll
-      for (int c = 0; c < 32; c++) {
-        float2 e = make_float2(x[2 * c], x[2 * c + 1]);
-        e = kForm == 0 ? __ffma2_rn(e, splat2(f.sl2), splat2(-base)) : __fadd2_rn(e, splat2(-base));
-        e.x = ex2(e.x);
-        e.y = ex2(e.y);
-        pk[c] = pack2(e.x, e.y);
-        part[c & 1] = __fadd2_rn(part[c & 1], e);
-        part_r[c & 1] = __fadd2_rn(part_r[c & 1], bf162_to_f2(pk[c]));
-      }
-      tc_st32(trow + (j & 1) * 64, pk);
+      // The probabilities go to the second half of the scores' columns: their second half first, whose scores are at hand.
+      uint32_t pk[16];
+      probabilities<kForm>(f, pc, a, test, see1, base, pk, sum, exact);
+      tc_st16(tS + 48, pk);
+      tc_ld32_issue(tS, a);
+      tc_ld32_wait(a);
+      pc = piece_of<kForm>(f, r, c0, a);
+      probabilities<kForm>(f, pc, a, test, see0, base, pk, sum, exact);
+      tc_st16(tS + 32, pk);
       tc_st_wait();
-      if ((entry & 1) && s.len < c0 + AM_COLS) {
+      if (test && s.len < c0 + AM_COLS) {
         if (!mbar_wait(smem_u32(&vfull[j % NS]), j / NS & 1, abort_flag, p.status)) { ok = false; break; }
-        clear_rows<DP>(Vs + (j % NS) * Sh::KV_BYTES, s.len - c0, threadIdx.x - 64);
+        clear_rows<DP, 32 * AF_SOFT>(Vs + (j % NS) * Sh::KV_BYTES, s.len - c0, threadIdx.x - 64);
         fence_proxy_async_smem();
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&pready[j & 1]));
-      exact += (part[0].x + part[0].y) + (part[1].x + part[1].y);
-      sum += (part_r[0].x + part_r[0].y) + (part_r[1].x + part_r[1].y);
     }
     if (ok && n > 0) ok = mbar_wait(smem_u32(&oall), 0, abort_flag, p.status);
     if (ok) {
       tc_fence_after();
-      const bool empty = r >= s.len || !(sum > 0.f);
+      const float total = sum.x + sum.y;
+      const bool empty = r >= s.len || !(total > 0.f);
       const long long at = b * p.o0.batch + r * p.o0.row + h * p.o0.head;
-      store_row<DP>(trow + O_COL, p.o0.p + at, p.rest ? p.rest + at : nullptr, empty ? 0.f : 1.f / sum, empty, n > 0, r < p.m.S, p.D);
+      store_row(trow + Sh::O_COL, p.o0.p + at, p.rest ? p.rest + at : nullptr, empty ? 0.f : 1.f / total, empty, n > 0, r < p.m.S, 0, DP, p.D);
       if (p.lse && r < p.m.S)
-        p.lse[((long long)b * p.heads + h) * p.m.S + r] = empty ? -INFINITY : (top + log2f(exact)) * LN2;
+        p.lse[((long long)b * p.heads + h) * p.m.S + r] = empty ? -INFINITY : (top + log2f(exact.x + exact.y)) * LN2;
     }
   }
   tc_fence_before();
@@ -560,7 +672,7 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
-    tmem_free<256>(tmem);
+    tmem_free<Sh::COLS>(tmem);
   }
 }
 
@@ -614,7 +726,7 @@ template <int DP, bool kKeys> struct BwdShape {
 // kKeys = false: rows are queries (A = q, B = k, C = dctx, D = v; loop over keys), the result is dq.
 // kKeys = true: rows are keys (A = k, B = q, C = v, D = dctx; loop over the queries of every head that shares them): dk, dv.
 template <int DP, bool kKeys, int kForm>
-__global__ void __launch_bounds__(AM_THREADS, DP == 64 ? 2 : 1)
+__global__ void __launch_bounds__(AB_THREADS, DP == 64 ? 2 : 1)
 masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
               const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmD, const TcParams p) {
   typedef BwdShape<DP, kKeys> Sh;
@@ -628,8 +740,7 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   __shared__ uint64_t fixfull, full[NS], empty[NS], sfull[2], ready[2], dpread, done;
   __shared__ uint32_t tmem_slot;
   __shared__ int red[16];
-  __shared__ __align__(16) int docs_of[AM_SOFT][AM_COLS];
-  __shared__ __align__(16) float cols_of[kKeys ? AM_SOFT : 1][2][AM_COLS];   // kKeys: lse (log2) and delta of the loop's queries
+  __shared__ __align__(16) float cols_of[kKeys ? AB_SOFT : 1][2][32];   // kKeys: -lse (log2) and -delta of a warp's queries
   __shared__ __align__(8) int flag_mem[4];
   volatile int* abort_flag = flag_mem + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -641,9 +752,9 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     }
     for (int i = 0; i < 2; i++) {
       mbar_init(smem_u32(&sfull[i]), 1);
-      mbar_init(smem_u32(&ready[i]), AM_SOFT);
+      mbar_init(smem_u32(&ready[i]), AB_SOFT);
     }
-    mbar_init(smem_u32(&dpread), AM_SOFT);
+    mbar_init(smem_u32(&dpread), AB_SOFT);
     mbar_init(smem_u32(&done), 1);
     *abort_flag = 0;
     *reinterpret_cast<volatile long long*>(abort_flag + 1) = p.wait_limit;
@@ -667,7 +778,7 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   const int tile = p.m.causal && !kKeys ? p.tiles - 1 - idx : idx;  // causal: the tiles with the longest loops start first
   const int r0 = tile * AM_ROWS;
   const Seq s = sequence(p.m, b);
-  const int n_list = list_blocks<kKeys>(p.m, s, b, r0, list, red);
+  const int n_list = list_blocks<kKeys, AB_THREADS / 32>(p.m, s, b, r0, list, red);
   const int n = kKeys ? n_list * group : n_list;
   // loop step j: its list entry and head
   auto entry_of = [&](int j) { return (int)list[kKeys ? j % n_list : j]; };
@@ -728,10 +839,10 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       tc_fence_after();
       const uint32_t at = tmem + (j % Sh::SB) * 64;
       if (kKeys) {
-        product_ts(tmem + Sh::ACC_COL, at, stage(j) + Sh::LOOP_BYTES, id_acc, j > 0);        // dV += P^T dC
-        product_ts(tmem + Sh::ACC_COL + DP, at + 32, stage(j), id_acc, j > 0);               // dK += dS^T Q
+        product_ts(tmem + Sh::ACC_COL, at, 32, stage(j) + Sh::LOOP_BYTES, id_acc, j > 0);    // dV += P^T dC
+        product_ts(tmem + Sh::ACC_COL + DP, at + 16, 32, stage(j), id_acc, j > 0);           // dK += dS^T Q
       } else {
-        product_ts(tmem + Sh::ACC_COL, at, stage(j), id_acc, j > 0);                         // dQ += dS K
+        product_ts(tmem + Sh::ACC_COL, at, 32, stage(j), id_acc, j > 0);                     // dQ += dS K
       }
       tc_commit(smem_u32(&empty[j % NS]));
       if (more && Sh::SB == 1) {
@@ -742,117 +853,90 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     if (ok) tc_commit(smem_u32(&done));
     if (!ok || *abort_flag) settle(&done);
   } else if (warp >= 2) {
-    // ------------------------------- softmax and its backward: a thread owns a row -------------------------------
-    const int quarter = warp & 3, row = quarter * 32 + lane, r = r0 + row;
-    const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16);
+    // ------------------ softmax and its backward: a thread owns half of a row's columns ------------------
+    const int quarter = warp & 3, half = (warp - 2) >> 2, r = r0 + quarter * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16) + half * 32;
     const int* docs = p.m.docs ? p.m.docs + (long long)b * p.m.S : nullptr;
     const int doc = docs && r < s.len ? docs[r] : 0;
-    Form f = form_of(p.m, kKeys ? hr * group : hr);
-    float lse2 = INFINITY, delta = 0.f;
-    if (!kKeys && r < s.len) {
-      const long long at = ((long long)b * p.heads + hr) * p.m.S + r;
-      lse2 = p.lse[at] * LOG2E;
-      delta = p.delta[at];
-    }
+    Form f = form_of<kForm>(p.m, kKeys ? hr * group : hr);
+    float lse2 = 0.f, delta = 0.f;   // of the row (queries), or of the lane's column of the next step (keys)
+    auto ask = [&](int h, int i) {
+      const long long at = ((long long)b * p.heads + h) * p.m.S + i;
+      lse2 = i < s.len ? p.lse[at] * LOG2E : 0.f;
+      delta = i < s.len ? p.delta[at] : 0.f;
+    };
+    if (!kKeys) ask(hr, r);
+    else if (n > 0) ask(hr * group, (entry_of(0) >> 1) * AM_COLS + half * 32 + lane);
     bool ok = true;
     for (int j = 0; j < n; j++) {
-      const int entry = entry_of(j), c0 = (entry >> 1) * AM_COLS;
-      uint64_t see = ~0ull;
-      if (kKeys || ((entry & 1) && docs)) {
+      const int entry = entry_of(j), c0 = (entry >> 1) * AM_COLS + half * 32;
+      const bool test = entry & 1;
+      if (kKeys) {
         __syncwarp();
-        if (kKeys) {
-          const int hq = head_of(j);
-          if (kForm == 2 || kForm == 1) f = form_of(p.m, hq);
-          const long long at = ((long long)b * p.heads + hq) * p.m.S + c0;
-#pragma unroll
-          for (int e = lane; e < 64; e += 32) {
-            const bool live = c0 + e < s.len;
-            cols_of[warp - 2][0][e] = live ? -p.lse[at + e] * LOG2E : 0.f;
-            cols_of[warp - 2][1][e] = live ? -p.delta[at + e] : 0.f;
-          }
-        }
-        if ((entry & 1) && docs) {
-          docs_of[warp - 2][lane] = c0 + lane < s.len ? docs[c0 + lane] : 0;
-          docs_of[warp - 2][lane + 32] = c0 + lane + 32 < s.len ? docs[c0 + lane + 32] : 0;
-        }
+        cols_of[warp - 2][0][lane] = -lse2;
+        cols_of[warp - 2][1][lane] = -delta;
         __syncwarp();
+        if (j + 1 < n) ask(head_of(j + 1), (entry_of(j + 1) >> 1) * AM_COLS + half * 32 + lane);
+        if (kForm == 1 || kForm == 2) f.slope2 = p.m.slopes ? p.m.slopes[head_of(j)] * LOG2E : 0.f;
       }
-      if (entry & 1) see = visible<kKeys>(s, r, c0, docs != nullptr, doc, docs_of[warp - 2]);
+      uint32_t see = ~0u;
+      if (test) see = visible<kKeys>(s, r, c0, docs, doc);
       if (!mbar_wait(smem_u32(&sfull[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
       tc_fence_after();
       const uint32_t tS = trow + (j % Sh::SB) * 64, tP = trow + Sh::DP_COL + (j % Sh::PB) * 64;
-      uint32_t pk[32];  // kKeys: P in the first half, dS in the second, 32 columns at a time
-      uint32_t keep[16];
-#pragma unroll
-      for (int half = 0; half < 2; half++) {
-        uint32_t a[32], d[32];
-        tc_ld32_issue(tS + half * 32, a);
-        tc_ld32_issue(tP + half * 32, d);
-        tc_ld32_wait(a);
-        tc_ld32_wait(d);
-        if (half == 1 && Sh::PB == 1) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&dpread));
-        }
-        const uint32_t w = (uint32_t)(see >> (32 * half));
-        const float off = (float)(c0 + half * 32 - r);
+      uint32_t a[32], d[32];
+      tc_ld32_issue(tS, a);
+      tc_ld32_issue(tP, d);
+      tc_ld32_wait(a);
+      tc_ld32_wait(d);
+      if (Sh::PB == 1) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&dpread));
+      }
+      const Piece pc = piece_of<kForm>(f, r, c0, a);
+      uint32_t pp[16], ds[16];
+      choose_way<kForm>(f, pc, test, [&](auto way) {
+        typedef decltype(way) Wy;
 #pragma unroll
         for (int c = 0; c < 32; c += 2) {
           float2 x = make_float2(__uint_as_float(a[c]), __uint_as_float(a[c + 1]));
           float2 t = make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
           float2 nl = splat2(-lse2), nd = splat2(-delta), bend = splat2(1.f);
           if (kKeys) {
-            nl = *reinterpret_cast<const float2*>(&cols_of[warp - 2][0][half * 32 + c]);
-            nd = *reinterpret_cast<const float2*>(&cols_of[warp - 2][1][half * 32 + c]);
+            nl = *reinterpret_cast<const float2*>(&cols_of[warp - 2][0][c]);
+            nd = *reinterpret_cast<const float2*>(&cols_of[warp - 2][1][c]);
           }
-          if (kForm == 0) {
-            x = __ffma2_rn(x, splat2(f.sl2), nl);
-          } else {
-            x.x = exponent<kForm>(f, x.x, fabsf(off + (float)c), &bend.x);
-            x.y = exponent<kForm>(f, x.y, fabsf(off + (float)(c + 1)), &bend.y);
-            x = __fadd2_rn(x, nl);
-          }
+          x = exponents<Wy, true>(f, pc, x, c, nl, &bend);
           x.x = ex2(x.x);
           x.y = ex2(x.y);
           t = __fmul2_rn(__fadd2_rn(t, nd), x);
-          if (kForm == 2) t = __fmul2_rn(t, bend);
-          if (entry & 1) {
+          if (Wy::CAP) t = __fmul2_rn(t, bend);
+          if (Wy::TEST) {
             // A row with a single key has no gradient by its score: dP - delta is the difference of two sums in different
-            // orders there, and is zero in truth.  p(dP_j - delta) is at most (1 - p) times the spread of dP, so
-            // nothing above 1e-5 of it is dropped; a block without pairs to test has 64 keys a row and no such p alone.
+            // orders there, and is zero in truth.  p(dP_j - delta) is at most (1 - p) times the spread of dP, so nothing
+            // above 1e-5 of it is dropped; a block without pairs to test has 64 keys a row and no such p alone.
             const bool one0 = x.x > 0.99999f, one1 = x.y > 0.99999f;
-            const bool v0 = w >> c & 1, v1 = w >> (c + 1) & 1;
+            const bool v0 = see >> c & 1, v1 = see >> (c + 1) & 1;
             x.x = v0 ? x.x : 0.f;
             x.y = v1 ? x.y : 0.f;
             t.x = v0 && !one0 ? t.x : 0.f;
             t.y = v1 && !one1 ? t.y : 0.f;
           }
-          if (kKeys) {
-            const int at = (half * 32 + c) / 2;
-            pk[at] = pack2(x.x, x.y);
-            if (half == 0) keep[at] = pack2(t.x, t.y);
-            else a[c / 2] = pack2(t.x, t.y);
-          } else {
-            pk[(half * 32 + c) / 2] = pack2(t.x, t.y);
-          }
+          if (kKeys) pp[c / 2] = pack2(x.x, x.y);
+          ds[c / 2] = pack2(t.x, t.y);
         }
-        if (kKeys && half == 1) {
-          uint32_t ds[32];
-#pragma unroll
-          for (int e = 0; e < 16; e++) {
-            ds[e] = keep[e];
-            ds[16 + e] = a[e];
-          }
-          tc_st32(tS + 32, ds);
-        }
-      }
-      tc_st32(tS, pk);
+      });
+      // over the scores that this warp has read: keys, P and then dS; queries, dS
+      if (kKeys) tc_st16(tS, pp);
+      tc_st16(kKeys ? tS + 16 : tS, ds);
       tc_st_wait();
-      if ((entry & 1) && s.len < c0 + AM_COLS) {
+      const int first = (entry >> 1) * AM_COLS;
+      if (test && s.len < first + AM_COLS) {
         // the products' reads of this stage so far are over (S and dP are complete); its rows are an operand once more
-        clear_rows<DP>(Bs + (j % NS) * 2 * Sh::LOOP_BYTES, s.len - c0, threadIdx.x - 64);
-        if (kKeys) clear_rows<DP>(Bs + (j % NS) * 2 * Sh::LOOP_BYTES + Sh::LOOP_BYTES, s.len - c0, threadIdx.x - 64);
+        uint8_t* tiles = Bs + (j % NS) * 2 * Sh::LOOP_BYTES;
+        clear_rows<DP, 32 * AB_SOFT>(tiles, s.len - first, threadIdx.x - 64);
+        if (kKeys) clear_rows<DP, 32 * AB_SOFT>(tiles + Sh::LOOP_BYTES, s.len - first, threadIdx.x - 64);
         fence_proxy_async_smem();
       }
       tc_fence_before();
@@ -862,14 +946,15 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     if (ok && n > 0) ok = mbar_wait(smem_u32(&done), 0, abort_flag, p.status);
     if (ok) {
       tc_fence_after();
-      const bool dead = r >= s.len;
-      const long long a0 = b * p.o0.batch + r * p.o0.row + hr * p.o0.head;
+      const bool dead = r >= s.len, write = r < p.m.S;
+      const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16) + Sh::ACC_COL;
       if (kKeys) {
-        const long long a1 = b * p.o1.batch + r * p.o1.row + hr * p.o1.head;
-        store_row<DP>(trow + Sh::ACC_COL, p.o1.p + a1, nullptr, 1.f, dead, n > 0, r < p.m.S, p.D);
-        store_row<DP>(trow + Sh::ACC_COL + DP, p.o0.p + a0, nullptr, p.m.scale, dead, n > 0, r < p.m.S, p.D);
+        const View& o = half ? p.o0 : p.o1;
+        store_row(acc + half * DP, o.p + (b * o.batch + r * o.row + hr * o.head), nullptr, half ? p.m.scale : 1.f, dead, n > 0, write, 0, DP,
+                  p.D);
       } else {
-        store_row<DP>(trow + Sh::ACC_COL, p.o0.p + a0, nullptr, p.m.scale, dead, n > 0, r < p.m.S, p.D);
+        store_row(acc, p.o0.p + (b * p.o0.batch + r * p.o0.row + hr * p.o0.head), nullptr, p.m.scale, dead, n > 0, write, half * (DP / 2),
+                  (half + 1) * (DP / 2), p.D);
       }
     }
   }
@@ -930,7 +1015,7 @@ template <int DP, int kForm>
 int forward(const mslt_attention_desc& d, TcParams& p, const MapVal* m, cudaStream_t st, char* err) {
   static bool done[kMaxDevices];
   if (opt_in(masked_fwd_tc<DP, kForm>, done, FwdShape<DP>::SMEM + kMostList, err)) return MSLT_ERR_CUDA;
-  launch_pdl(masked_fwd_tc<DP, kForm>, d.B * d.heads * p.tiles, AM_THREADS, FwdShape<DP>::SMEM + list_bytes(d.S), st, m[0].map, m[1].map,
+  launch_pdl(masked_fwd_tc<DP, kForm>, d.B * d.heads * p.tiles, AF_THREADS, FwdShape<DP>::SMEM + list_bytes(d.S), st, m[0].map, m[1].map,
              m[2].map, p);
   return 0;
 }
@@ -939,7 +1024,7 @@ int backward(const mslt_attention_desc& d, TcParams& p, const MapVal* m, cudaStr
   static bool done[kMaxDevices];
   typedef BwdShape<DP, kKeys> Sh;
   if (opt_in(masked_bwd_tc<DP, kKeys, kForm>, done, Sh::SMEM + kMostList, err)) return MSLT_ERR_CUDA;
-  launch_pdl(masked_bwd_tc<DP, kKeys, kForm>, d.B * (kKeys ? d.kv_heads : d.heads) * p.tiles, AM_THREADS, Sh::SMEM + list_bytes(d.S), st,
+  launch_pdl(masked_bwd_tc<DP, kKeys, kForm>, d.B * (kKeys ? d.kv_heads : d.heads) * p.tiles, AB_THREADS, Sh::SMEM + list_bytes(d.S), st,
              m[0].map, m[1].map, m[2].map, m[3].map, p);
   return 0;
 }
