@@ -36,14 +36,18 @@ bool attn_take_starve();  // whether the next attention launch was asked to run 
 namespace {
 
 constexpr int AM_ROWS = 128;      // rows of a block
-constexpr int AM_COLS = 64;       // rows of a loop block
+constexpr int AF_COLS = 64, AB_COLS = 128;  // rows of a loop block, forward and backward
 constexpr int AF_SOFT = 4, AF_THREADS = 64 + 32 * AF_SOFT;  // forward: softmax warps, threads
-constexpr int AB_SOFT = 8, AB_THREADS = 64 + 32 * AB_SOFT;  // backward
+constexpr int AB_SOFT = 16, AB_THREADS = 64 + 32 * AB_SOFT;  // backward
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-// The running maximum of a row is followed only where it grows by more than 2^8: until then the probabilities stay
-// below 2^8, which costs bf16 nothing, and the accumulator in tensor memory need not be read and written.
-constexpr float AM_SLACK = 8.0f;
-
+// A row's exponents are relative to a reference: the largest score of the first block in which it sees anything, without its
+// bias, rounded up to a whole number (capped scores: none).  Later blocks take no maximum: range is what counts and not
+// size, and a row whose probabilities do not add up to something between 2^-64 and 2^90 is the rare exception.  A block with
+// such a row goes over its loop again, this time with a running maximum; the reference then moves by whole powers of two,
+// so what is there so far is scaled without rounding.  (With a running maximum throughout, a loop block of four
+// blocks an SM spent 550 of 2900 cycles on it, and its scores were read a third time; sums tested against the limit block
+// by block still cost 450 cycles of a block alone on its SM, 85 of 940 of the SM.)
+constexpr float AM_MOST = 1.2379400392853803e27f, AM_LEAST = 5.421010862427522e-20f;  // 2^90, 2^-64
 
 struct View { bf16* p; long long batch, row, head; };
 struct TcParams {
@@ -74,14 +78,24 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16])
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+__device__ __forceinline__ void tc_ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
         "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr)
       : "memory");
+}
+__device__ __forceinline__ void tc_ld16_wait(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  tc_ld16_issue(taddr, r);
+  tc_ld16_wait(r);
 }
 __device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -100,6 +114,16 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// acc += the two bf16 of h, in fp32: one instruction each, where unpacking takes two more
+__device__ __forceinline__ void add_bf16(float2& acc, uint32_t h) {
+  asm("{\n\t.reg .b16 lo, hi;\n\t"
+      "mov.b32 {lo, hi}, %2;\n\t"
+      "add.f32.bf16 %0, lo, %0;\n\t"
+      "add.f32.bf16 %1, hi, %1;\n\t}"
+      : "+f"(acc.x), "+f"(acc.y)
+      : "r"(h));
+}
+
 // ---- which loop blocks a row tile visits --------------------------------------------------------------
 
 struct Seq { int len, prefix; };
@@ -112,7 +136,7 @@ __device__ __forceinline__ Seq sequence(const AttnMask& m, int b) {
 
 // Called by the whole block.  list[i] receives 2 * block + (pairs to test); returns their number.  Rows r0 .. r0 + 127 are
 // queries (and the blocks keys), or with kKeys the other way round.  red: 16 words of shared memory.
-template <bool kKeys, int kWarps>
+template <bool kKeys, int kWarps, int kCols>
 __device__ __forceinline__ int list_blocks(const AttnMask& m, const Seq& s, int b, int r0, uint16_t* list, int* red) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int* docs = m.docs ? m.docs + (long long)b * m.S : nullptr;
@@ -133,33 +157,39 @@ __device__ __forceinline__ int list_blocks(const AttnMask& m, const Seq& s, int 
   int first = 0, last = 0;
   if (r0 < s.len) {
     last = kKeys ? s.len : min(s.len, max(r1 + 1, s.prefix));
-    first = kKeys && r0 >= s.prefix ? r0 / AM_COLS : 0;
-    last = (last + AM_COLS - 1) / AM_COLS;
+    first = kKeys && r0 >= s.prefix ? r0 / kCols : 0;
+    last = (last + kCols - 1) / kCols;
   }
   // whole by positions: every pair of live rows counts
   auto whole = [&](int c0) {
-    if (c0 + AM_COLS > s.len) return false;
-    return kKeys ? (c0 >= r1 || r1 < s.prefix) : (c0 + AM_COLS - 1 <= r0 || c0 + AM_COLS <= s.prefix);
+    if (c0 + kCols > s.len) return false;
+    return kKeys ? (c0 >= r1 || r1 < s.prefix) : (c0 + kCols - 1 <= r0 || c0 + kCols <= s.prefix);
   };
   if (docs) {
-    constexpr int kAhead = 4;  // blocks whose documents are asked for together
+    constexpr int kAhead = 256 / kCols;  // blocks whose documents are asked for together
     for (int base = first + warp; base < last; base += kWarps * kAhead) {
-      int d0[kAhead], d1[kAhead];
+      int d[kAhead][kCols / 32];
+#pragma unroll
+      for (int u = 0; u < kAhead; u++)
+#pragma unroll
+        for (int e = 0; e < kCols / 32; e++) {
+          const int c = (base + u * kWarps) * kCols + 32 * e + lane;
+          d[u][e] = c < s.len ? docs[c] : 0;
+        }
 #pragma unroll
       for (int u = 0; u < kAhead; u++) {
-        const int c = (base + u * kWarps) * AM_COLS + lane;
-        d0[u] = c < s.len ? docs[c] : 0;
-        d1[u] = c + 32 < s.len ? docs[c + 32] : 0;
-      }
+        const int blk = base + u * kWarps;
+        int mn = 0x7fffffff, mx = (int)0x80000000;
 #pragma unroll
-      for (int u = 0; u < kAhead; u++) {
-        const int blk = base + u * kWarps, c = blk * AM_COLS + lane;
-        int mn = min(c < s.len ? d0[u] : 0x7fffffff, c + 32 < s.len ? d1[u] : 0x7fffffff);
-        int mx = max(c < s.len ? d0[u] : (int)0x80000000, c + 32 < s.len ? d1[u] : (int)0x80000000);
+        for (int e = 0; e < kCols / 32; e++)
+          if (blk * kCols + 32 * e + lane < s.len) {
+            mn = min(mn, d[u][e]);
+            mx = max(mx, d[u][e]);
+          }
         mn = __reduce_min_sync(0xffffffffu, mn);
         mx = __reduce_max_sync(0xffffffffu, mx);
         if (lane == 0 && blk < last)
-          list[blk] = mn > hi || mx < lo ? 0 : (lo == hi && mn == lo && mx == lo && whole(blk * AM_COLS)) ? 1 : 2;
+          list[blk] = mn > hi || mx < lo ? 0 : (lo == hi && mn == lo && mx == lo && whole(blk * kCols)) ? 1 : 2;
       }
     }
     __syncthreads();
@@ -169,7 +199,7 @@ __device__ __forceinline__ int list_blocks(const AttnMask& m, const Seq& s, int 
     for (int base = first; base < last; base += 32) {
       const int blk = base + lane;
       int kind = 0;
-      if (blk < last) kind = docs ? list[blk] : whole(blk * AM_COLS) ? 1 : 2;
+      if (blk < last) kind = docs ? list[blk] : whole(blk * kCols) ? 1 : 2;
       const uint32_t take = __ballot_sync(0xffffffffu, kind != 0);
       __syncwarp();
       if (kind) list[n + __popc(take & ((1u << lane) - 1))] = (uint16_t)(blk * 2 + (kind == 2));
@@ -236,20 +266,20 @@ __device__ __forceinline__ Form form_of(const AttnMask& m, int h) {
   }
   return f;
 }
-// A warp's piece of 32 columns: what is the same for all of it.  side: 0 the distance of pairs needs its absolute value, 1
+// A warp's piece of 32 (or 16) columns: what is the same for all of it.  side: 0 the distance of pairs needs its absolute value, 1
 // all columns lie before all rows of the warp, -1 behind; then the bias is linear in the column.
 struct Piece { float off; int side; bool small; };
-template <int kForm>
-__device__ __forceinline__ Piece piece_of(const Form& f, int r, int c0, const uint32_t (&s)[32]) {
+template <int kForm, int N>
+__device__ __forceinline__ Piece piece_of(const Form& f, int r, int c0, const uint32_t (&s)[N]) {
   Piece p;
   p.off = (float)(c0 - r);
   const int r_first = r - (int)(threadIdx.x & 31);
-  p.side = c0 + 31 <= r_first ? 1 : c0 >= r_first + 31 ? -1 : 0;
+  p.side = c0 + N - 1 <= r_first ? 1 : c0 >= r_first + 31 ? -1 : 0;
   p.small = true;
   if (kForm == 2) {
     float m = 0.f;
 #pragma unroll
-    for (int c = 0; c < 32; c += 2) m = fmaxf(m, fmaxf(fabsf(__uint_as_float(s[c])), fabsf(__uint_as_float(s[c + 1]))));
+    for (int c = 0; c < N; c += 2) m = fmaxf(m, fmaxf(fabsf(__uint_as_float(s[c])), fabsf(__uint_as_float(s[c + 1]))));
     p.small = __all_sync(0xffffffffu, m <= f.small);
   }
   return p;
@@ -318,13 +348,14 @@ __device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t a_kb
       tc_mma(d, ad, bd, idesc, kb + k > 0 ? 1u : 0u);
     }
 }
-// D (+)= A B, A 64 wide in tensor memory (its second half `a_half` columns behind the first), B 64 rows (the
-// contraction) of DP contiguous elements
-__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t a_half, uint32_t b, uint32_t idesc, uint32_t accumulate) {
-  const uint32_t hi = (uint32_t)(make_smem_desc(0, 16) >> 32), lo = (uint32_t)make_smem_desc(0, 8192);
+// D (+)= A B over kRows rows of B, each of DP contiguous elements.  A lies in tensor memory, 32 of the contraction in 16
+// columns, the next 32 `a_step` columns on.
+template <int kRows>
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t a_step, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+  const uint32_t hi = (uint32_t)(make_smem_desc(0, 16) >> 32), lo = (uint32_t)make_smem_desc(0, kRows * 128);
 #pragma unroll
-  for (int k = 0; k < 4; k++)
-    tc_mma_ts(d, a + (k >> 1) * a_half + (k & 1) * 8, ((uint64_t)hi << 32) | (lo + addr16(b) + k * 128), idesc, accumulate | (k > 0));
+  for (int k = 0; k < kRows / 16; k++)
+    tc_mma_ts(d, a + (k >> 1) * a_step + (k & 1) * 8, ((uint64_t)hi << 32) | (lo + addr16(b) + k * 128), idesc, accumulate | (k > 0));
 }
 
 template <int DP>
@@ -345,13 +376,13 @@ __device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
   while (!mbar_try_wait(smem_u32(bar), parity) && now_cycles() - t0 < 200000000ll) {}
 }
 
-// Rows `from` .. 63 of a loop block's tiles become zero; the whole softmax group, thread t of kThreads.
-template <int DP, int kThreads>
+// Rows `from` on of a loop block's tiles of kRows rows become zero; the whole softmax group, thread t of kThreads.
+template <int DP, int kRows, int kThreads>
 __device__ __forceinline__ void clear_rows(uint8_t* tile, int from, int t) {
 #pragma unroll
   for (int kb = 0; kb < DP / 64; kb++)
-    for (int v = from * 8 + t; v < AM_COLS * 8; v += kThreads)
-      reinterpret_cast<uint4*>(tile + kb * 8192)[v] = make_uint4(0, 0, 0, 0);
+    for (int v = from * 8 + t; v < kRows * 8; v += kThreads)
+      reinterpret_cast<uint4*>(tile + kb * kRows * 128)[v] = make_uint4(0, 0, 0, 0);
 }
 
 // Columns [c0, c1) of a row of an accumulator, scaled, to bf16 in memory (from dst on), 16 at a time; optionally what the
@@ -413,7 +444,7 @@ __device__ __forceinline__ void settle(uint64_t* bar) {
 template <int DP> struct FwdShape {
   static constexpr int BLOCKS = DP == 64 ? 4 : 2, SB = DP == 64 ? 1 : 2, STAGES = 2;
   static constexpr int COLS = DP == 64 ? 128 : 256, O_COL = SB * 64;
-  static constexpr int Q_BYTES = AM_ROWS * DP * 2, KV_BYTES = AM_COLS * DP * 2;
+  static constexpr int Q_BYTES = AM_ROWS * DP * 2, KV_BYTES = AF_COLS * DP * 2;
   static constexpr int SMEM = Q_BYTES + 2 * STAGES * KV_BYTES;
 };
 
@@ -435,17 +466,18 @@ __device__ __forceinline__ void probabilities(const Form& f, const Piece& pc, co
       e.y = ex2(e.y);
       pk[c / 2] = pack2(e.x, e.y);
       exact = __fadd2_rn(exact, e);
-      sum = __fadd2_rn(sum, bf162_to_f2(pk[c / 2]));
+      add_bf16(sum, pk[c / 2]);
     }
   });
 }
 // Upper bound of the exponents of 32 columns that a row sees (-infinity: none), near enough to the largest to be the
 // reference of the row's exponents: without a bias it is the largest, with one it is above by at most 31 slopes, which
-// costs nothing but range while a slope is at most one power of two (a larger one is taken element by element).
+// costs nothing but range while a slope is at most one power of two (a larger one is taken element by element).  unbiased:
+// as if the pairs were at distance 0, which bounds blocks to come too.
 template <int kForm>
-__device__ __forceinline__ float largest(const Form& f, const Piece& pc, const uint32_t (&s)[32], bool test, uint32_t see) {
+__device__ __forceinline__ float largest(const Form& f, const Piece& pc, const uint32_t (&s)[32], bool test, uint32_t see, bool unbiased) {
   float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  if (kForm == 0 || (kForm == 1 && f.sl2 > 0.f && f.slope2 >= 0.f && f.slope2 <= 1.f)) {
+  if (kForm == 0 || (kForm == 1 && f.sl2 > 0.f && f.slope2 >= 0.f && (unbiased || f.slope2 <= 1.f))) {
     if (test) {
 #pragma unroll
       for (int c = 0; c < 32; c += 2) {
@@ -457,7 +489,7 @@ __device__ __forceinline__ float largest(const Form& f, const Piece& pc, const u
       for (int c = 0; c < 32; c += 2) m[c >> 1 & 3] = fmaxf(m[c >> 1 & 3], fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
     }
     const float big = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * f.sl2;
-    if (kForm == 0) return big;
+    if (kForm == 0 || unbiased) return big;
     return big - f.slope2 * (pc.off > 0.f ? pc.off : fmaxf(0.f, -31.f - pc.off));
   }
   choose_way<kForm>(f, pc, test, [&](auto way) {
@@ -526,146 +558,172 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   const int tile = p.m.causal ? p.tiles - 1 - idx : idx;  // causal: the tiles with the most keys start first
   const int hk = h / (p.heads / p.kv_heads), r0 = tile * AM_ROWS;
   const Seq s = sequence(p.m, b);
-  const int n = list_blocks<false, AF_THREADS / 32>(p.m, s, b, r0, list, red);
+  const int n = list_blocks<false, AF_THREADS / 32, AF_COLS>(p.m, s, b, r0, list, red);
 
-  if (warp == 0 && n > 0 && !p.starve && elect_one()) {
-    // ------------------------------- TMA producer -------------------------------
-    mbar_expect_tx(smem_u32(&qfull), Sh::Q_BYTES);
-    load_rows<DP>(smem_u32(smem), &tmQ, p.a_perm, smem_u32(&qfull), r0, h, b, 16384);
-    int k_issued = 0, v_issued = 0;
-    for (int j = 0; j < n; j++) {
-      const int st = j % NS, row = (list[j] >> 1) * AM_COLS;
-      const uint32_t par = (uint32_t)(j / NS & 1) ^ 1;
-      if (!mbar_wait(smem_u32(&kempty[st]), par, abort_flag, p.status)) break;
-      mbar_expect_tx(smem_u32(&kfull[st]), Sh::KV_BYTES);
-      load_rows<DP>(smem_u32(Ks + st * Sh::KV_BYTES), &tmK, p.b_perm, smem_u32(&kfull[st]), row, hk, b, 8192);
-      k_issued = j + 1;
-      if (!mbar_wait(smem_u32(&vempty[st]), par, abort_flag, p.status)) break;
-      mbar_expect_tx(smem_u32(&vfull[st]), Sh::KV_BYTES);
-      load_rows<DP>(smem_u32(Vs + st * Sh::KV_BYTES), &tmV, p.c_perm, smem_u32(&vfull[st]), row, hk, b, 8192);
-      v_issued = j + 1;
-    }
-    if (v_issued < n || *abort_flag) {
-      drain(&qfull, 0);
-      for (int j = max(0, k_issued - NS); j < k_issued; j++) drain(&kfull[j % NS], (j / NS) & 1);
-      for (int j = max(0, v_issued - NS); j < v_issued; j++) drain(&vfull[j % NS], (j / NS) & 1);
-    }
-  } else if (warp == 1 && n > 0 && elect_one()) {
-    // ------------------------------- products -------------------------------
-    constexpr uint32_t id_s = idesc_of(AM_COLS, false), id_o = idesc_of(DP, true);
-    auto scores = [&](int j) {
-      const int st = j % NS;
-      if (!mbar_wait(smem_u32(&kfull[st]), j / NS & 1, abort_flag, p.status)) return false;
-      tc_fence_after();
-      product_ss<DP>(tmem + (j % SB) * 64, smem_u32(smem), 1024, smem_u32(Ks + st * Sh::KV_BYTES), 512, id_s);
-      tc_commit(smem_u32(&sfull[j & 1]));
-      tc_commit(smem_u32(&kempty[st]));
-      return true;
-    };
-    bool ok = mbar_wait(smem_u32(&qfull), 0, abort_flag, p.status) && scores(0);
-    for (int j = 0; j < n && ok; j++) {
-      if (SB == 2 && j + 1 < n && !scores(j + 1)) { ok = false; break; }
-      const int st = j % NS;
-      ok = mbar_wait(smem_u32(&vfull[st]), j / NS & 1, abort_flag, p.status) &&
-           mbar_wait(smem_u32(&pready[j & 1]), j >> 1 & 1, abort_flag, p.status);
-      if (!ok) break;
-      tc_fence_after();
-      product_ts(tmem + Sh::O_COL, tmem + (j % SB) * 64 + 32, 16, smem_u32(Vs + st * Sh::KV_BYTES), id_o, j > 0);
-      if (SB == 2) tc_commit(smem_u32(&odone[j & 1]));
-      tc_commit(smem_u32(&vempty[st]));
-      // one buffer: the probabilities lie in it until the product with V, issued before, has read them
-      if (SB == 1 && j + 1 < n && !scores(j + 1)) { ok = false; break; }
-    }
-    if (ok) tc_commit(smem_u32(&oall));
-    if (!ok || *abort_flag) settle(&oall);
-  } else if (warp >= 2) {
-    // ------------------------------- softmax: a thread owns a query -------------------------------
-    const int quarter = warp & 3, r = r0 + quarter * 32 + lane;
-    const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16);
-    const Form f = form_of<kForm>(p.m, h);
-    const int* docs = p.m.docs ? p.m.docs + (long long)b * p.m.S : nullptr;
-    const int doc = docs && r < s.len ? docs[r] : 0;
-    // Capped scores lie in [-cap, cap]: a cap of up to 44 (2^64) needs no reference, and the exponentials' range holds.
-    const bool fixed = kForm == 2 && f.cap2 <= 64.f && f.slope2 == 0.f;
-    float top = fixed ? 0.f : -INFINITY;                                  // reference of the row's exponents
-    float2 sum = make_float2(0.f, 0.f), exact = make_float2(0.f, 0.f);   // of the rounded probabilities, and of the unrounded ones
-    bool ok = true;
-    for (int j = 0; j < n; j++) {
-      const int entry = list[j], c0 = (entry >> 1) * AM_COLS;
-      const bool test = entry & 1;
-      uint32_t see0 = ~0u, see1 = ~0u;
-      if (test) {
-        see0 = visible<false>(s, r, c0, docs, doc);
-        see1 = visible<false>(s, r, c0 + 32, docs, doc);
+  // state of a softmax thread, which owns a query
+  const int quarter = warp & 3, r = r0 + quarter * 32 + lane;
+  const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16);
+  const Form f = form_of<kForm>(p.m, h);
+  const int* docs = p.m.docs ? p.m.docs + (long long)b * p.m.S : nullptr;
+  const int doc = docs && r < s.len ? docs[r] : 0;
+  // Capped scores lie in [-cap, cap]: a cap of up to 44 (2^64) needs no reference.
+  const bool fixed = kForm == 2 && f.cap2 <= 64.f && f.slope2 >= 0.f;
+  float top = 0.f;                                                      // reference of the row's exponents, a whole number
+  float2 sum = make_float2(0.f, 0.f), exact = make_float2(0.f, 0.f);   // of the rounded probabilities, and of the unrounded ones
+  bool ok = true;
+
+  // Steps are counted on through both goes over the loop, so that the barriers' phases go on too.
+  for (int go = 0; go < 2 && n > 0; go++) {
+    const int j0 = go * n, j1 = j0 + n;
+    bool again = false;
+    if (warp == 0 && !p.starve && elect_one()) {
+      // ------------------------------- TMA producer -------------------------------
+      if (go == 0) {
+        mbar_expect_tx(smem_u32(&qfull), Sh::Q_BYTES);
+        load_rows<DP>(smem_u32(smem), &tmQ, p.a_perm, smem_u32(&qfull), r0, h, b, 16384);
       }
-      if (!mbar_wait(smem_u32(&sfull[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
-      tc_fence_after();
-      const uint32_t tS = trow + (j % SB) * 64;
-      uint32_t a[32];
-      float big = -INFINITY;
-      if (!fixed) {
-        tc_ld32_issue(tS, a);
-        tc_ld32_wait(a);
-        big = largest<kForm>(f, piece_of<kForm>(f, r, c0, a), a, test, see0);
+      int k_issued = j0, v_issued = j0;
+      for (int j = j0; j < j1; j++) {
+        const int st = j % NS, row = (list[j - j0] >> 1) * AF_COLS;
+        const uint32_t par = (uint32_t)(j / NS & 1) ^ 1;
+        if (!mbar_wait(smem_u32(&kempty[st]), par, abort_flag, p.status)) break;
+        mbar_expect_tx(smem_u32(&kfull[st]), Sh::KV_BYTES);
+        load_rows<DP>(smem_u32(Ks + st * Sh::KV_BYTES), &tmK, p.b_perm, smem_u32(&kfull[st]), row, hk, b, 8192);
+        k_issued = j + 1;
+        if (!mbar_wait(smem_u32(&vempty[st]), par, abort_flag, p.status)) break;
+        mbar_expect_tx(smem_u32(&vfull[st]), Sh::KV_BYTES);
+        load_rows<DP>(smem_u32(Vs + st * Sh::KV_BYTES), &tmV, p.c_perm, smem_u32(&vfull[st]), row, hk, b, 8192);
+        v_issued = j + 1;
       }
-      tc_ld32_issue(tS + 32, a);
-      tc_ld32_wait(a);
-      Piece pc = piece_of<kForm>(f, r, c0 + 32, a);
-      if (!fixed) {
-        big = fmaxf(big, largest<kForm>(f, pc, a, test, see1));
-        const bool grow = big > top + AM_SLACK || (top == -INFINITY && big > top);
-        if (__any_sync(0xffffffffu, grow)) {
-          const float by = grow ? ex2(top - big) : 1.f;
-          if (grow) top = big;
-          sum = __fmul2_rn(sum, splat2(by));
-          exact = __fmul2_rn(exact, splat2(by));
-          if (j > 0) {
-            // The accumulator of the blocks so far.  One buffer of scores: they were issued behind the last product with V.
-            // Two: the scores at hand only say that the product before the last is complete, hence two barriers, so that
-            // neither can be a phase ahead.
-            if (SB == 2 && !mbar_wait(smem_u32(&odone[(j - 1) & 1]), (j - 1) >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
+      if (v_issued < j1 || *abort_flag) {
+        drain(&qfull, 0);
+        for (int j = max(0, k_issued - NS); j < k_issued; j++) drain(&kfull[j % NS], (j / NS) & 1);
+        for (int j = max(0, v_issued - NS); j < v_issued; j++) drain(&vfull[j % NS], (j / NS) & 1);
+      }
+    } else if (warp == 1 && elect_one()) {
+      // ------------------------------- products -------------------------------
+      constexpr uint32_t id_s = idesc_of(AF_COLS, false), id_o = idesc_of(DP, true);
+      auto landed = [&](uint64_t* bar, int j) { return mbar_wait(smem_u32(&bar[j % NS]), j / NS & 1, abort_flag, p.status); };
+      auto scores = [&](int j) {
+        const int st = j % NS;
+        product_ss<DP>(tmem + (j % SB) * 64, smem_u32(smem), 1024, smem_u32(Ks + st * Sh::KV_BYTES), 512, id_s);
+        tc_commit(smem_u32(&sfull[j & 1]));
+        tc_commit(smem_u32(&kempty[st]));
+      };
+      // What is not the probabilities is waited for ahead of them: from their arrival to the next scores there is one wait.
+      bool fine = mbar_wait(smem_u32(&qfull), 0, abort_flag, p.status) && landed(kfull, j0);
+      if (fine) {
+        tc_fence_after();
+        scores(j0);
+      }
+      for (int j = j0; j < j1 && fine; j++) {
+        const int st = j % NS;
+        if (j + 1 < j1) {
+          if (!landed(kfull, j + 1)) { fine = false; break; }
+          if (SB == 2) {
             tc_fence_after();
-#pragma unroll 1
-            for (int c = 0; c < DP; c += 16) {
-              uint32_t o[16];
-              tc_ld16(trow + Sh::O_COL + c, o);
-#pragma unroll
-              for (int e = 0; e < 16; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-              tc_st16(trow + Sh::O_COL + c, o);
-            }
+            scores(j + 1);
           }
         }
+        fine = landed(vfull, j) && mbar_wait(smem_u32(&pready[j & 1]), j >> 1 & 1, abort_flag, p.status);
+        if (!fine) break;
+        tc_fence_after();
+        product_ts<AF_COLS>(tmem + Sh::O_COL, tmem + (j % SB) * 64, 16, smem_u32(Vs + st * Sh::KV_BYTES), id_o, j > j0);
+        if (SB == 2) tc_commit(smem_u32(&odone[j & 1]));
+        // one buffer: the probabilities lie in it until the product with V, issued before, has read them
+        if (SB == 1 && j + 1 < j1) scores(j + 1);
+        tc_commit(smem_u32(&vempty[st]));
       }
-      const float base = top == -INFINITY ? 0.f : top;
-      // The probabilities go to the second half of the scores' columns: their second half first, whose scores are at hand.
-      uint32_t pk[16];
-      probabilities<kForm>(f, pc, a, test, see1, base, pk, sum, exact);
-      tc_st16(tS + 48, pk);
-      tc_ld32_issue(tS, a);
-      tc_ld32_wait(a);
-      pc = piece_of<kForm>(f, r, c0, a);
-      probabilities<kForm>(f, pc, a, test, see0, base, pk, sum, exact);
-      tc_st16(tS + 32, pk);
-      tc_st_wait();
-      if (test && s.len < c0 + AM_COLS) {
-        if (!mbar_wait(smem_u32(&vfull[j % NS]), j / NS & 1, abort_flag, p.status)) { ok = false; break; }
-        clear_rows<DP, 32 * AF_SOFT>(Vs + (j % NS) * Sh::KV_BYTES, s.len - c0, threadIdx.x - 64);
-        fence_proxy_async_smem();
+      if (fine) tc_commit(smem_u32(&oall));
+      if (!fine || *abort_flag) settle(&oall);
+    } else if (warp >= 2) {
+      // ------------------------------- softmax -------------------------------
+      bool settled = fixed && go == 0;  // every row of the warp has its reference
+      top = settled || r >= s.len ? 0.f : -INFINITY;
+      sum = exact = make_float2(0.f, 0.f);
+      uint32_t seen = 0;
+      for (int j = j0; j < j1; j++) {
+        const int entry = list[j - j0], c0 = (entry >> 1) * AF_COLS;
+        const bool test = entry & 1;
+        uint32_t see[2] = {~0u, ~0u};
+        if (test) {
+          see[0] = visible<false>(s, r, c0, docs, doc);
+          see[1] = visible<false>(s, r, c0 + 32, docs, doc);
+        }
+        seen |= see[0] | see[1];
+        if (!mbar_wait(smem_u32(&sfull[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t tS = trow + (j % SB) * 64;
+        uint32_t a[32];
+        if (!settled) {
+          float big = -INFINITY;
+#pragma unroll
+          for (int half = 0; half < 2; half++) {
+            tc_ld32_issue(tS + 32 * half, a);
+            tc_ld32_wait(a);
+            big = fmaxf(big, largest<kForm>(f, piece_of<kForm>(f, r, c0 + 32 * half, a), a, test, see[half], go == 0));
+          }
+          float up = 0.f;
+          if (top == -INFINITY) top = ceilf(big);   // has seen nothing yet: sums and accumulator are zero
+          else if (go == 1 && big > top) up = ceilf(big - top);
+          if (go == 1 && __any_sync(0xffffffffu, up > 0.f)) {
+            const float by = ex2(-up);
+            top += up;
+            sum = __fmul2_rn(sum, splat2(by));
+            exact = __fmul2_rn(exact, splat2(by));
+            if (j > j0) {
+              // The accumulator of the blocks so far.  One buffer of scores: they were issued behind the last product with V.
+              // Two: the scores at hand only say that the product before the last is complete, hence two barriers, so that
+              // neither can be a phase ahead.
+              if (SB == 2 && !mbar_wait(smem_u32(&odone[(j - 1) & 1]), (j - 1) >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < DP; c += 16) {
+                uint32_t o[16];
+                tc_ld16(trow + Sh::O_COL + c, o);
+#pragma unroll
+                for (int e = 0; e < 16; e++) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                tc_st16(trow + Sh::O_COL + c, o);
+              }
+            }
+          }
+          settled = go == 0 && __all_sync(0xffffffffu, top != -INFINITY);
+        }
+        const float base = top == -INFINITY ? 0.f : top;
+        // The probabilities of a half take 16 columns of the scores that were read for the half.
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+          tc_ld32_issue(tS + 32 * half, a);
+          tc_ld32_wait(a);
+          uint32_t pk[16];
+          probabilities<kForm>(f, piece_of<kForm>(f, r, c0 + 32 * half, a), a, test, see[half], base, pk, sum, exact);
+          tc_st16(tS + 16 * half, pk);
+        }
+        tc_st_wait();
+        if (test && s.len < c0 + AF_COLS) {
+          if (!mbar_wait(smem_u32(&vfull[j % NS]), j / NS & 1, abort_flag, p.status)) { ok = false; break; }
+          clear_rows<DP, AF_COLS, 32 * AF_SOFT>(Vs + (j % NS) * Sh::KV_BYTES, s.len - c0, threadIdx.x - 64);
+          fence_proxy_async_smem();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&pready[j & 1]));
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&pready[j & 1]));
+      if (ok) ok = mbar_wait(smem_u32(&oall), go, abort_flag, p.status);
+      const float total = exact.x + exact.y;
+      again = ok && seen && r < s.len && !(total >= AM_LEAST && total <= AM_MOST);
     }
-    if (ok && n > 0) ok = mbar_wait(smem_u32(&oall), 0, abort_flag, p.status);
-    if (ok) {
-      tc_fence_after();
-      const float total = sum.x + sum.y;
-      const bool empty = r >= s.len || !(total > 0.f);
-      const long long at = b * p.o0.batch + r * p.o0.row + h * p.o0.head;
-      store_row(trow + Sh::O_COL, p.o0.p + at, p.rest ? p.rest + at : nullptr, empty ? 0.f : 1.f / total, empty, n > 0, r < p.m.S, 0, DP, p.D);
-      if (p.lse && r < p.m.S)
-        p.lse[((long long)b * p.heads + h) * p.m.S + r] = empty ? -INFINITY : (top + log2f(exact.x + exact.y)) * LN2;
-    }
+    if (!__syncthreads_or(again) || *abort_flag) break;
+  }
+
+  if (warp >= 2 && ok) {
+    tc_fence_after();
+    const float total = sum.x + sum.y;
+    const bool empty = r >= s.len || !(total > 0.f);
+    const long long at = b * p.o0.batch + r * p.o0.row + h * p.o0.head;
+    store_row(trow + Sh::O_COL, p.o0.p + at, p.rest ? p.rest + at : nullptr, empty ? 0.f : 1.f / total, empty, n > 0, r < p.m.S, 0, DP, p.D);
+    if (p.lse && r < p.m.S)
+      p.lse[((long long)b * p.heads + h) * p.m.S + r] = empty ? -INFINITY : (top + log2f(exact.x + exact.y)) * LN2;
   }
   tc_fence_before();
   __syncthreads();
@@ -711,22 +769,22 @@ masked_delta_tc(const View dc, const View c, const bf16* rest, float* delta, int
   if (n < rows && e == 0) delta[(b * heads + h) * S + i] = sum;
 }
 
-// Tensor memory and stages of the two backward kernels.  Heads of up to 64: 256 columns, two blocks an SM.  Wider
-// ones need 384 and more, so one block an SM has two buffers of S and dP and its products run ahead of the softmax.
+// Tensor memory and stages of the two backward kernels: S 128 columns, dP 128, the accumulators DP or 2 DP.  S has a second
+// buffer, so that the next block's products run under this block's softmax, but for dK and dV of heads wider than 64, which
+// fill the 512 columns.
 template <int DP, bool kKeys> struct BwdShape {
-  static constexpr bool wide = DP == 128;
-  static constexpr int SB = wide || !kKeys ? 2 : 1, PB = wide ? 2 : 1;   // buffers of S, of dP
-  static constexpr int STAGES = wide ? 4 : 3;
-  static constexpr int COLS = wide ? 512 : 256;
-  static constexpr int DP_COL = SB * 64, ACC_COL = DP_COL + PB * 64;
-  static constexpr int FIX_BYTES = AM_ROWS * DP * 2, LOOP_BYTES = AM_COLS * DP * 2;
+  static constexpr int SB = DP == 128 && kKeys ? 1 : 2;
+  static constexpr int STAGES = DP == 128 ? 2 : 4;
+  static constexpr int COLS = 512;
+  static constexpr int DP_COL = SB * 128, ACC_COL = DP_COL + 128;
+  static constexpr int FIX_BYTES = AM_ROWS * DP * 2, LOOP_BYTES = AB_COLS * DP * 2;
   static constexpr int SMEM = 2 * FIX_BYTES + STAGES * 2 * LOOP_BYTES;
 };
 
 // kKeys = false: rows are queries (A = q, B = k, C = dctx, D = v; loop over keys), the result is dq.
 // kKeys = true: rows are keys (A = k, B = q, C = v, D = dctx; loop over the queries of every head that shares them): dk, dv.
 template <int DP, bool kKeys, int kForm>
-__global__ void __launch_bounds__(AB_THREADS, DP == 64 ? 2 : 1)
+__global__ void __launch_bounds__(AB_THREADS, 1)
 masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
               const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmD, const TcParams p) {
   typedef BwdShape<DP, kKeys> Sh;
@@ -778,7 +836,7 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   const int tile = p.m.causal && !kKeys ? p.tiles - 1 - idx : idx;  // causal: the tiles with the longest loops start first
   const int r0 = tile * AM_ROWS;
   const Seq s = sequence(p.m, b);
-  const int n_list = list_blocks<kKeys, AB_THREADS / 32>(p.m, s, b, r0, list, red);
+  const int n_list = list_blocks<kKeys, AB_THREADS / 32, AB_COLS>(p.m, s, b, r0, list, red);
   const int n = kKeys ? n_list * group : n_list;
   // loop step j: its list entry and head
   auto entry_of = [&](int j) { return (int)list[kKeys ? j % n_list : j]; };
@@ -792,12 +850,12 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     load_rows<DP>(smem_u32(Cs), &tmC, p.c_perm, fb, r0, hr, b, 16384);
     int issued = 0;
     for (int j = 0; j < n; j++) {
-      const int st = j % NS, row = (entry_of(j) >> 1) * AM_COLS, hl = head_of(j);
+      const int st = j % NS, row = (entry_of(j) >> 1) * AB_COLS, hl = head_of(j);
       if (!mbar_wait(smem_u32(&empty[st]), (uint32_t)(j / NS & 1) ^ 1, abort_flag, p.status)) break;
       const uint32_t bar = smem_u32(&full[st]), dst = smem_u32(Bs + st * 2 * Sh::LOOP_BYTES);
       mbar_expect_tx(bar, 2 * Sh::LOOP_BYTES);
-      load_rows<DP>(dst, &tmB, p.b_perm, bar, row, hl, b, 8192);
-      load_rows<DP>(dst + Sh::LOOP_BYTES, &tmD, p.d_perm, bar, row, hl, b, 8192);
+      load_rows<DP>(dst, &tmB, p.b_perm, bar, row, hl, b, 16384);
+      load_rows<DP>(dst + Sh::LOOP_BYTES, &tmD, p.d_perm, bar, row, hl, b, 16384);
       issued = j + 1;
     }
     if (issued < n || *abort_flag) {
@@ -806,16 +864,16 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     }
   } else if (warp == 1 && n > 0 && elect_one()) {
     // ------------------------------- products -------------------------------
-    constexpr uint32_t id_s = idesc_of(AM_COLS, false), id_acc = idesc_of(DP, true);
+    constexpr uint32_t id_s = idesc_of(AB_COLS, false), id_acc = idesc_of(DP, true);
     auto stage = [&](int j) { return smem_u32(Bs + (j % NS) * 2 * Sh::LOOP_BYTES); };
     auto landed = [&](int j) {
       if (!mbar_wait(smem_u32(&full[j % NS]), j / NS & 1, abort_flag, p.status)) return false;
       tc_fence_after();
       return true;
     };
-    auto scores = [&](int j) { product_ss<DP>(tmem + (j % Sh::SB) * 64, smem_u32(As), 1024, stage(j), 512, id_s); };
+    auto scores = [&](int j) { product_ss<DP>(tmem + (j % Sh::SB) * 128, smem_u32(As), 1024, stage(j), 1024, id_s); };
     auto dprobs = [&](int j) {
-      product_ss<DP>(tmem + Sh::DP_COL + (j % Sh::PB) * 64, smem_u32(Cs), 1024, stage(j) + Sh::LOOP_BYTES, 512, id_s);
+      product_ss<DP>(tmem + Sh::DP_COL, smem_u32(Cs), 1024, stage(j) + Sh::LOOP_BYTES, 1024, id_s);
     };
     bool ok = mbar_wait(smem_u32(&fixfull), 0, abort_flag, p.status) && landed(0);
     if (ok) {
@@ -828,84 +886,101 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       if (more) {
         if (!landed(j + 1)) { ok = false; break; }
         if (Sh::SB == 2) scores(j + 1);
-        if (Sh::PB == 1) {
-          if (!mbar_wait(smem_u32(&dpread), j & 1, abort_flag, p.status)) { ok = false; break; }
-          tc_fence_after();
-        }
+        if (!mbar_wait(smem_u32(&dpread), j & 1, abort_flag, p.status)) { ok = false; break; }
+        tc_fence_after();
         dprobs(j + 1);
         if (Sh::SB == 2) tc_commit(smem_u32(&sfull[(j + 1) & 1]));
       }
       if (!mbar_wait(smem_u32(&ready[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
       tc_fence_after();
-      const uint32_t at = tmem + (j % Sh::SB) * 64;
+      const uint32_t at = tmem + (j % Sh::SB) * 128;
       if (kKeys) {
-        product_ts(tmem + Sh::ACC_COL, at, 32, stage(j) + Sh::LOOP_BYTES, id_acc, j > 0);    // dV += P^T dC
-        product_ts(tmem + Sh::ACC_COL + DP, at + 16, 32, stage(j), id_acc, j > 0);           // dK += dS^T Q
+        product_ts<AB_COLS>(tmem + Sh::ACC_COL, at, 32, stage(j) + Sh::LOOP_BYTES, id_acc, j > 0);    // dV += P^T dC
+        product_ts<AB_COLS>(tmem + Sh::ACC_COL + DP, at + 16, 32, stage(j), id_acc, j > 0);           // dK += dS^T Q
       } else {
-        product_ts(tmem + Sh::ACC_COL, at, 32, stage(j), id_acc, j > 0);                     // dQ += dS K
+        product_ts<AB_COLS>(tmem + Sh::ACC_COL, at, 32, stage(j), id_acc, j > 0);                     // dQ += dS K
       }
-      tc_commit(smem_u32(&empty[j % NS]));
       if (more && Sh::SB == 1) {
         scores(j + 1);
         tc_commit(smem_u32(&sfull[(j + 1) & 1]));
       }
+      tc_commit(smem_u32(&empty[j % NS]));
     }
     if (ok) tc_commit(smem_u32(&done));
     if (!ok || *abort_flag) settle(&done);
   } else if (warp >= 2) {
-    // ------------------ softmax and its backward: a thread owns half of a row's columns ------------------
-    const int quarter = warp & 3, half = (warp - 2) >> 2, r = r0 + quarter * 32 + lane;
-    const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16) + half * 32;
+    // ------------------ softmax and its backward: a thread owns 32 columns of a row ------------------
+    const int quarter = warp & 3, part = (warp - 2) >> 2, r = r0 + quarter * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16) + part * 32;
     const int* docs = p.m.docs ? p.m.docs + (long long)b * p.m.S : nullptr;
     const int doc = docs && r < s.len ? docs[r] : 0;
     Form f = form_of<kForm>(p.m, kKeys ? hr * group : hr);
-    float lse2 = 0.f, delta = 0.f;   // of the row (queries), or of the lane's column of the next step (keys)
+    // lse and delta: of the row (queries), or of the lane's column of the next step (keys).  Those are asked for a step ahead and
+    // not touched before they are needed (multiplied where they were asked for, they cost 1000 of 2700 cycles a step).
+    float lse = 0.f, delta = 0.f;
     auto ask = [&](int h, int i) {
       const long long at = ((long long)b * p.heads + h) * p.m.S + i;
-      lse2 = i < s.len ? p.lse[at] * LOG2E : 0.f;
-      delta = i < s.len ? p.delta[at] : 0.f;
+      lse = delta = 0.f;
+      if (i < s.len) {
+        lse = p.lse[at];
+        delta = p.delta[at];
+      }
     };
     if (!kKeys) ask(hr, r);
-    else if (n > 0) ask(hr * group, (entry_of(0) >> 1) * AM_COLS + half * 32 + lane);
+    else if (n > 0) ask(hr * group, (list[0] >> 1) * AB_COLS + part * 32 + lane);
+    const float lse2 = lse * LOG2E;
+    int at_list = 0, head = kKeys ? hr * group : hr / group;  // of step j
     bool ok = true;
     for (int j = 0; j < n; j++) {
-      const int entry = entry_of(j), c0 = (entry >> 1) * AM_COLS + half * 32;
+      const int entry = list[at_list], c0 = (entry >> 1) * AB_COLS + part * 32;
       const bool test = entry & 1;
       if (kKeys) {
         __syncwarp();
-        cols_of[warp - 2][0][lane] = -lse2;
+        cols_of[warp - 2][0][lane] = -lse * LOG2E;
         cols_of[warp - 2][1][lane] = -delta;
         __syncwarp();
-        if (j + 1 < n) ask(head_of(j + 1), (entry_of(j + 1) >> 1) * AM_COLS + half * 32 + lane);
-        if (kForm == 1 || kForm == 2) f.slope2 = p.m.slopes ? p.m.slopes[head_of(j)] * LOG2E : 0.f;
+        if (kForm == 1 || kForm == 2) f.slope2 = p.m.slopes ? p.m.slopes[head] * LOG2E : 0.f;
       }
+      if (++at_list == n_list) {
+        at_list = 0;
+        head++;
+      }
+      if (kKeys && j + 1 < n) ask(head, (list[at_list] >> 1) * AB_COLS + part * 32 + lane);
       uint32_t see = ~0u;
       if (test) see = visible<kKeys>(s, r, c0, docs, doc);
       if (!mbar_wait(smem_u32(&sfull[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
       tc_fence_after();
-      const uint32_t tS = trow + (j % Sh::SB) * 64, tP = trow + Sh::DP_COL + (j % Sh::PB) * 64;
-      uint32_t a[32], d[32];
-      tc_ld32_issue(tS, a);
-      tc_ld32_issue(tP, d);
-      tc_ld32_wait(a);
-      tc_ld32_wait(d);
-      if (Sh::PB == 1) {
+      const uint32_t tS = trow + (j % Sh::SB) * 128, tP = trow + Sh::DP_COL;
+      uint32_t pp[16], ds[16];
+#pragma unroll
+      for (int q = 0; q < 32; q += 16) {  // 16 columns at a time: 32 need more than the 96 registers that 576 threads have
+      uint32_t a[16], d[16];
+      tc_ld16_issue(tS + q, a);
+      tc_ld16_issue(tP + q, d);
+      tc_ld16_wait(a);
+      tc_ld16_wait(d);
+      if (q) {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&dpread));
       }
-      const Piece pc = piece_of<kForm>(f, r, c0, a);
-      uint32_t pp[16], ds[16];
+      const Piece pc = piece_of<kForm>(f, r, c0 + q, a);
+      const uint32_t seen = see >> q;
       choose_way<kForm>(f, pc, test, [&](auto way) {
         typedef decltype(way) Wy;
+        float4 nl4, nd4;
 #pragma unroll
-        for (int c = 0; c < 32; c += 2) {
+        for (int c = 0; c < 16; c += 2) {
           float2 x = make_float2(__uint_as_float(a[c]), __uint_as_float(a[c + 1]));
           float2 t = make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
           float2 nl = splat2(-lse2), nd = splat2(-delta), bend = splat2(1.f);
           if (kKeys) {
-            nl = *reinterpret_cast<const float2*>(&cols_of[warp - 2][0][c]);
-            nd = *reinterpret_cast<const float2*>(&cols_of[warp - 2][1][c]);
+            if (c % 4 == 0) {
+              nl4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][0][q + c]);
+              nd4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][1][q + c]);
+            }
+            nl = c % 4 ? make_float2(nl4.z, nl4.w) : make_float2(nl4.x, nl4.y);
+            nd = c % 4 ? make_float2(nd4.z, nd4.w) : make_float2(nd4.x, nd4.y);
           }
           x = exponents<Wy, true>(f, pc, x, c, nl, &bend);
           x.x = ex2(x.x);
@@ -917,26 +992,27 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             // orders there, and is zero in truth.  p(dP_j - delta) is at most (1 - p) times the spread of dP, so nothing
             // above 1e-5 of it is dropped; a block without pairs to test has 64 keys a row and no such p alone.
             const bool one0 = x.x > 0.99999f, one1 = x.y > 0.99999f;
-            const bool v0 = see >> c & 1, v1 = see >> (c + 1) & 1;
+            const bool v0 = seen >> c & 1, v1 = seen >> (c + 1) & 1;
             x.x = v0 ? x.x : 0.f;
             x.y = v1 ? x.y : 0.f;
             t.x = v0 && !one0 ? t.x : 0.f;
             t.y = v1 && !one1 ? t.y : 0.f;
           }
-          if (kKeys) pp[c / 2] = pack2(x.x, x.y);
-          ds[c / 2] = pack2(t.x, t.y);
+          if (kKeys) pp[(q + c) / 2] = pack2(x.x, x.y);
+          ds[(q + c) / 2] = pack2(t.x, t.y);
         }
       });
+      }
       // over the scores that this warp has read: keys, P and then dS; queries, dS
       if (kKeys) tc_st16(tS, pp);
       tc_st16(kKeys ? tS + 16 : tS, ds);
       tc_st_wait();
-      const int first = (entry >> 1) * AM_COLS;
-      if (test && s.len < first + AM_COLS) {
+      const int first = (entry >> 1) * AB_COLS;
+      if (test && s.len < first + AB_COLS) {
         // the products' reads of this stage so far are over (S and dP are complete); its rows are an operand once more
         uint8_t* tiles = Bs + (j % NS) * 2 * Sh::LOOP_BYTES;
-        clear_rows<DP, 32 * AB_SOFT>(tiles, s.len - first, threadIdx.x - 64);
-        if (kKeys) clear_rows<DP, 32 * AB_SOFT>(tiles + Sh::LOOP_BYTES, s.len - first, threadIdx.x - 64);
+        clear_rows<DP, AB_COLS, 32 * AB_SOFT>(tiles, s.len - first, threadIdx.x - 64);
+        if (kKeys) clear_rows<DP, AB_COLS, 32 * AB_SOFT>(tiles + Sh::LOOP_BYTES, s.len - first, threadIdx.x - 64);
         fence_proxy_async_smem();
       }
       tc_fence_before();
@@ -949,12 +1025,13 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       const bool dead = r >= s.len, write = r < p.m.S;
       const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16) + Sh::ACC_COL;
       if (kKeys) {
-        const View& o = half ? p.o0 : p.o1;
-        store_row(acc + half * DP, o.p + (b * o.batch + r * o.row + hr * o.head), nullptr, half ? p.m.scale : 1.f, dead, n > 0, write, 0, DP,
-                  p.D);
+        const int which = part >> 1;  // 0: dV, 1: dK
+        const View& o = which ? p.o0 : p.o1;
+        store_row(acc + which * DP, o.p + (b * o.batch + r * o.row + hr * o.head), nullptr, which ? p.m.scale : 1.f, dead, n > 0, write,
+                  (part & 1) * (DP / 2), ((part & 1) + 1) * (DP / 2), p.D);
       } else {
-        store_row(acc, p.o0.p + (b * p.o0.batch + r * p.o0.row + hr * p.o0.head), nullptr, p.m.scale, dead, n > 0, write, half * (DP / 2),
-                  (half + 1) * (DP / 2), p.D);
+        store_row(acc, p.o0.p + (b * p.o0.batch + r * p.o0.row + hr * p.o0.head), nullptr, p.m.scale, dead, n > 0, write, part * (DP / 4),
+                  (part + 1) * (DP / 4), p.D);
       }
     }
   }
@@ -1008,8 +1085,8 @@ TcParams params_of(const mslt_attention_desc& d, int* status, bool starve) {
 }
 int form_index(const mslt_attention_desc& d) { return d.cap > 0.f ? 2 : d.slopes || !(d.scale > 0.f) ? 1 : 0; }
 // shared memory beside the tiles: alignment and the list of blocks.  The largest list (S = 131072) is opted in for.
-size_t list_bytes(int S) { return 1024 + ((size_t)(S + AM_COLS - 1) / AM_COLS * 2 + 15) / 16 * 16; }
-constexpr size_t kMostList = 1024 + 131072 / AM_COLS * 2;
+size_t list_bytes(int S) { return 1024 + ((size_t)(S + AF_COLS - 1) / AF_COLS * 2 + 15) / 16 * 16; }
+constexpr size_t kMostList = 1024 + 131072 / AF_COLS * 2;
 
 template <int DP, int kForm>
 int forward(const mslt_attention_desc& d, TcParams& p, const MapVal* m, cudaStream_t st, char* err) {
@@ -1044,8 +1121,8 @@ int attn_masked_tc_fwd(const mslt_attention_desc& d, int* status, cudaStream_t s
   TcParams p = params_of(d, status, attn_take_starve());
   MapVal m[3];
   int rc = map_of(d.q, d, d.heads, AM_ROWS, &m[0], p.a_perm, err);
-  if (!rc) rc = map_of(d.k, d, d.kv_heads, AM_COLS, &m[1], p.b_perm, err);
-  if (!rc) rc = map_of(d.v, d, d.kv_heads, AM_COLS, &m[2], p.c_perm, err);
+  if (!rc) rc = map_of(d.k, d, d.kv_heads, AF_COLS, &m[1], p.b_perm, err);
+  if (!rc) rc = map_of(d.v, d, d.kv_heads, AF_COLS, &m[2], p.c_perm, err);
   if (rc) return rc;
   p.o0 = view_of(d.ctx);
   const int form = form_index(d);
@@ -1059,13 +1136,13 @@ int attn_masked_tc_bwd(const mslt_attention_desc& d, float* delta, int* status, 
   MapVal mq[4], mk[4];
   TcParams pk = p;
   int rc = map_of(d.q, d, d.heads, AM_ROWS, &mq[0], p.a_perm, err);
-  if (!rc) rc = map_of(d.k, d, d.kv_heads, AM_COLS, &mq[1], p.b_perm, err);
+  if (!rc) rc = map_of(d.k, d, d.kv_heads, AB_COLS, &mq[1], p.b_perm, err);
   if (!rc) rc = map_of(d.dctx, d, d.heads, AM_ROWS, &mq[2], p.c_perm, err);
-  if (!rc) rc = map_of(d.v, d, d.kv_heads, AM_COLS, &mq[3], p.d_perm, err);
+  if (!rc) rc = map_of(d.v, d, d.kv_heads, AB_COLS, &mq[3], p.d_perm, err);
   if (!rc) rc = map_of(d.k, d, d.kv_heads, AM_ROWS, &mk[0], pk.a_perm, err);
-  if (!rc) rc = map_of(d.q, d, d.heads, AM_COLS, &mk[1], pk.b_perm, err);
+  if (!rc) rc = map_of(d.q, d, d.heads, AB_COLS, &mk[1], pk.b_perm, err);
   if (!rc) rc = map_of(d.v, d, d.kv_heads, AM_ROWS, &mk[2], pk.c_perm, err);
-  if (!rc) rc = map_of(d.dctx, d, d.heads, AM_COLS, &mk[3], pk.d_perm, err);
+  if (!rc) rc = map_of(d.dctx, d, d.heads, AB_COLS, &mk[3], pk.d_perm, err);
   if (rc) return rc;
   int log_lanes = 0;
   while ((8 << log_lanes) < d.head_dim) log_lanes++;
