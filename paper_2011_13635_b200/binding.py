@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional
 
 import numpy as np
@@ -169,13 +170,14 @@ lib.mslt_op_attention_lse_bwd.argtypes = [_P, _P, _P, _P, _P, _P, C.c_int32, C.c
 lib.mslt_op_colsum.argtypes = [C.c_int32, _P, C.c_int64, C.c_int32, C.c_int32, _P, _P, C.c_int32]
 
 lib.mslt_rope_turns.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_int32, _P, C.POINTER(C.c_float)]
-lib.mslt_op_rope.argtypes = [C.POINTER(RopeDesc), _P, C.c_int32]
-lib.mslt_op_qk_norm_rope.argtypes = [C.POINTER(QkNormDesc), _P, C.c_int32]
-lib.mslt_op_qk_norm_rope_bwd.argtypes = [C.POINTER(QkNormDesc), _P, C.c_size_t, _P, C.c_int32]
+# the descriptors of these calls are passed as packed bytes or by reference
+lib.mslt_op_rope.argtypes = [_P, _P, C.c_int32]
+lib.mslt_op_qk_norm_rope.argtypes = [_P, _P, C.c_int32]
+lib.mslt_op_qk_norm_rope_bwd.argtypes = [_P, _P, C.c_size_t, _P, C.c_int32]
 lib.mslt_op_qk_norm_rope_bwd_scratch_bytes.restype = C.c_size_t
 lib.mslt_op_qk_norm_rope_bwd_scratch_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
-lib.mslt_op_attention_masked.argtypes = [C.POINTER(AttentionDesc), _P, _P, C.c_int32]
-lib.mslt_op_attention_masked_bwd.argtypes = [C.POINTER(AttentionDesc), _P, C.c_size_t, _P, _P, C.c_int32]
+lib.mslt_op_attention_masked.argtypes = [_P, _P, _P, C.c_int32]
+lib.mslt_op_attention_masked_bwd.argtypes = [_P, _P, C.c_size_t, _P, _P, C.c_int32]
 lib.mslt_op_attention_masked_bwd_scratch_bytes.restype = C.c_size_t
 lib.mslt_op_attention_masked_bwd_scratch_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
 
@@ -322,54 +324,84 @@ def mslt_op_colsum(x, n: int, out, stream: int, sync: bool = True) -> None:
 
 # -- positions and masks of the encoder's attention -------------------------------------------------
 # These take views (any strides that are multiples of 16 bytes, elements of a head side by side) and check what the
-# library cannot see: shapes, types, devices.
+# library cannot see: shapes, types, devices.  They are called for sequences of a few tokens too, where the host's time
+# is the call's: the descriptors are packed at once (a tree of ctypes structures takes 4 us more), a tensor is looked at
+# once, and torch is looked up once a process.
+
+_torch = None
+_one_device = False
+
+
+def _need_torch():
+    global _torch, _one_device
+    if _torch is None:
+        import torch
+        _one_device = torch.cuda.device_count() == 1
+        _torch = torch
+    return _torch
+
 
 def _refuse(what: str, text: str):
     raise MsltError(-1, f"{what}: {text}")
 
 
-def _same(what: str, ref, shape, dtype=None, **tensors):
-    """Each tensor (None passes) has this shape and type, lies on ref's device, and ends in neighbouring elements."""
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if tuple(t.shape) != tuple(shape):
-            _refuse(what, f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
-        if t.dtype != (dtype or ref.dtype):
-            _refuse(what, f"{name} is {t.dtype}, needs {dtype or ref.dtype}")
-        if t.device != ref.device:
-            _refuse(what, f"{name} is on {t.device}, needs {ref.device}")
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
-            _refuse(what, f"the last dimension of {name} must be contiguous")
+def _explain(what, name, t, shape, dtype, dev):
+    if tuple(t.shape) != tuple(shape):
+        _refuse(what, f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+    if t.dtype != dtype:
+        _refuse(what, f"{name} is {t.dtype}, needs {dtype}")
+    if t.get_device() != dev:
+        _refuse(what, f"{name} is on {t.device}, needs device {dev}")
+    _refuse(what, f"the last dimension of {name} must be contiguous")
 
 
-def _table(what: str, ref, shape, dtype, **tensors):
-    """As _same, and contiguous."""
-    _same(what, ref, shape, dtype, **tensors)
-    for name, t in tensors.items():
-        if t is not None and not t.is_contiguous():
-            _refuse(what, f"{name} must be contiguous")
+def _view(what, name, t, shape, dtype, dev):
+    """(address, strides) of a view of this shape and type on this device, its last dimension contiguous."""
+    st = t.stride()
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or (st[-1] != 1 and shape[-1] > 1):
+        _explain(what, name, t, shape, dtype, dev)
+    return t.data_ptr(), st
 
 
-def _call(ref, fn, *args):
-    """Runs fn with ref's device current: a stream belongs to its device."""
-    import torch
-    if ref.device.index == torch.cuda.current_device():
-        _check(fn(*args))
+def _table(what, name, t, shape, dtype, dev):
+    """Address of a contiguous tensor, 0 for None."""
+    if t is None:
+        return 0
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        _explain(what, name, t, shape, dtype, dev)
+    if not t.is_contiguous():
+        _refuse(what, f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _call(dev, fn, *args):
+    """Runs fn with device dev current: a stream belongs to its device."""
+    if _one_device or dev == _torch.cuda.current_device():
+        rc = fn(*args)
     else:
-        with torch.cuda.device(ref.device):
-            _check(fn(*args))
+        with _torch.cuda.device(dev):
+            rc = fn(*args)
+    if rc:
+        _check(rc)
 
 
-def _float_or_bf16(what: str, name: str, t, dims: int):
-    import torch
-    if t.dim() != dims or t.dtype not in (torch.float32, torch.bfloat16):
+def _first(what, name, t, dims):
+    """(type index, torch type, device) of the tensor that decides them."""
+    torch = _need_torch()
+    dtype, dev = t.dtype, t.get_device()
+    if t.dim() != dims or (dtype is not torch.bfloat16 and dtype is not torch.float32):
         _refuse(what, f"{name} needs {dims} dimensions and float32 or bfloat16")
-    if not t.is_cuda:
+    if dev < 0:
         raise MsltError(-4, f"{what}: {name} is not on a CUDA device: this library has no CPU path")
+    return int(dtype is torch.bfloat16), dtype, dev
 
 
 ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}
+# the fields of mslt_rope_desc, mslt_qk_norm_desc and mslt_attention_desc, with the compiler's padding
+_ROPE = struct.Struct("@4iPqqPqqP3iPfi")
+_NORM = struct.Struct("@4iPqqPqqP3iPfi2ifPPPqqPqqPP")
+_ATTN = struct.Struct("@6i" + "Pqqq" * 4 + "PP" + "Pqqq" * 4 + "ffPiPPP")
+assert (_ROPE.size, _NORM.size, _ATTN.size) == (C.sizeof(RopeDesc), C.sizeof(QkNormDesc), C.sizeof(AttentionDesc))
 
 
 def mslt_rope_turns(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained_len: int = 512):
@@ -383,42 +415,39 @@ def mslt_rope_turns(rot_dim: int, base: float = 10000.0, scaling: str = "none", 
     return turns, m.value
 
 
-def _rope_desc(what, x, y, turns, positions, seq, interleaved, magnitude, inverse) -> RopeDesc:
-    import torch
-    _float_or_bf16(what, "x", x, 3)
-    rows, heads, dim = x.shape
-    _same(what, x, x.shape, y=y)
+def _rope_fields(what, x, y, turns, positions, seq, interleaved, magnitude, inverse):
+    """The packed fields of mslt_rope_desc, x's shape, type and device."""
+    kind, dtype, dev = _first(what, "x", x, 3)
+    shape = x.shape
+    rows, heads, dim = shape
+    px, sx = _view(what, "x", x, shape, dtype, dev)
+    py, sy = (0, (0, 0)) if y is None else _view(what, "y", y, shape, dtype, dev)
     rot = 0 if turns is None else 2 * turns.shape[0]
-    if turns is not None:
-        _table(what, x, (rot // 2,), torch.int64, turns=turns)
-    _table(what, x, (rows,), torch.int32, positions=positions)
-    return RopeDesc(_dt(x), rows, heads, dim, x.data_ptr(), x.stride(0), x.stride(1), _ptr(y), 0 if y is None else y.stride(0),
-                    0 if y is None else y.stride(1), _ptr(positions), seq, rot, int(interleaved), _ptr(turns), magnitude, int(inverse))
+    return (kind, rows, heads, dim, px, sx[0], sx[1], py, sy[0], sy[1],
+            _table(what, "positions", positions, (rows,), _torch.int32, dev), seq, rot, bool(interleaved),
+            _table(what, "turns", turns, (rot // 2,), _torch.int64, dev), magnitude, bool(inverse)), shape, dtype, dev
 
 
 def mslt_op_rope(x, y, turns, stream: int, positions=None, seq: int = 0, interleaved: bool = False, magnitude: float = 1.0,
                  inverse: bool = False, sync: bool = True) -> None:
     """x, y [rows, heads, head_dim] float or bf16 (y may be x); turns int64 [rot_dim / 2] from mslt_rope_turns;
     positions int32 [rows] or None (row t at t % seq): CUDA tensors."""
-    d = _rope_desc("rope", x, y, turns, positions, seq, interleaved, magnitude, inverse)
-    _call(x, lib.mslt_op_rope, C.byref(d), stream, int(sync))
-
-
-def _norm_desc(what, x, y, gain, turns, q_heads, eps, bias, center, positions, seq, interleaved, magnitude) -> QkNormDesc:
-    import torch
-    rope = _rope_desc(what, x, y, turns, positions, seq, interleaved, magnitude, False)
-    _table(what, x, (2, x.shape[2]), torch.float32, gain=gain, bias=bias)
-    return QkNormDesc(rope, q_heads, int(center), eps, gain.data_ptr(), _ptr(bias))
+    f, _, _, dev = _rope_fields("rope", x, y, turns, positions, seq, interleaved, magnitude, inverse)
+    _call(dev, lib.mslt_op_rope, _ROPE.pack(*f), stream, sync)
 
 
 def mslt_op_qk_norm_rope(x, y, gain, turns, q_heads: int, eps: float, stream: int, bias=None, center: bool = False, positions=None,
                          seq: int = 0, interleaved: bool = False, magnitude: float = 1.0, sync: bool = True) -> None:
     """x, y, positions as in mslt_op_rope (turns None: no rotation); gain, bias fp32 [2, head_dim]: row 0 for the first
     q_heads heads, row 1 for the others; bias may be None."""
-    d = _norm_desc("qk_norm_rope", x, y, gain, turns, q_heads, eps, bias, center, positions, seq, interleaved, magnitude)
+    what = "qk_norm_rope"
     if y is None:
-        _refuse("qk_norm_rope", "y is None")
-    _call(x, lib.mslt_op_qk_norm_rope, C.byref(d), stream, int(sync))
+        _refuse(what, "y is None")
+    f, shape, _, dev = _rope_fields(what, x, y, turns, positions, seq, interleaved, magnitude, False)
+    wide = (2, shape[2])
+    d = _NORM.pack(*f, q_heads, bool(center), eps, _table(what, "gain", gain, wide, _torch.float32, dev),
+                   _table(what, "bias", bias, wide, _torch.float32, dev), 0, 0, 0, 0, 0, 0, 0, 0)
+    _call(dev, lib.mslt_op_qk_norm_rope, d, stream, sync)
 
 
 def mslt_op_qk_norm_rope_bwd_scratch_bytes(rows: int, heads: int, head_dim: int) -> int:
@@ -430,47 +459,57 @@ def mslt_op_qk_norm_rope_bwd(dy, x, dx, gain, dgain, turns, q_heads: int, eps: f
                              magnitude: float = 1.0, sync: bool = True) -> None:
     """dy, x, dx [rows, heads, head_dim] (dx may be dy); x is the forward's input; dgain, dbias (or None) fp32
     [2, head_dim] are written; scratch uint8."""
-    import torch
     what = "qk_norm_rope_bwd"
-    d = _norm_desc(what, x, None, gain, turns, q_heads, eps, None, center, positions, seq, interleaved, magnitude)
-    _same(what, x, x.shape, dy=dy, dx=dx)
-    _table(what, x, (2, x.shape[2]), torch.float32, dgain=dgain, dbias=dbias)
-    _table(what, x, scratch.shape, torch.uint8, scratch=scratch)
-    d.dy, d.dy_row, d.dy_head = dy.data_ptr(), dy.stride(0), dy.stride(1)
-    d.dx, d.dx_row, d.dx_head = dx.data_ptr(), dx.stride(0), dx.stride(1)
-    d.dgain, d.dbias = dgain.data_ptr(), _ptr(dbias)
-    _call(x, lib.mslt_op_qk_norm_rope_bwd, C.byref(d), scratch.data_ptr(), scratch.numel(), stream, int(sync))
+    f, shape, dtype, dev = _rope_fields(what, x, None, turns, positions, seq, interleaved, magnitude, False)
+    wide, f32 = (2, shape[2]), _torch.float32
+    pdy, sdy = _view(what, "dy", dy, shape, dtype, dev)
+    pdx, sdx = _view(what, "dx", dx, shape, dtype, dev)
+    d = _NORM.pack(*f, q_heads, bool(center), eps, _table(what, "gain", gain, wide, f32, dev), 0, pdy, sdy[0], sdy[1], pdx, sdx[0],
+                   sdx[1], _table(what, "dgain", dgain, wide, f32, dev), _table(what, "dbias", dbias, wide, f32, dev))
+    _call(dev, lib.mslt_op_qk_norm_rope_bwd, d, _table(what, "scratch", scratch, scratch.shape, _torch.uint8, dev), scratch.numel(),
+          stream, sync)
 
 
-def _heads(t) -> Heads:
-    return Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+def _attention_fields(what, q, k, v, ctx, lse, status, rest):
+    """The packed fields of mslt_attention_desc up to lse, the shapes of q and k, type and device."""
+    kind, dtype, dev = _first(what, "q", q, 4)
+    torch = _torch
+    shape = q.shape
+    B, S, heads, dim = shape
+    kshape = k.shape
+    if len(kshape) != 4 or kshape[0] != B or kshape[1] != S or kshape[3] != dim:
+        _explain(what, "k", k, (B, S, "kv_heads", dim), dtype, dev)
+    pq, sq = _view(what, "q", q, shape, dtype, dev)
+    pk, sk = _view(what, "k", k, kshape, dtype, dev)
+    pv, sv = _view(what, "v", v, kshape, dtype, dev)
+    pc, sc = _view(what, "ctx", ctx, shape, dtype, dev)
+    pr = 0
+    if rest is not None:
+        pr, sr = _view(what, "rest", rest, shape, dtype, dev)
+        if sr != sc:
+            _refuse(what, "rest must have the strides of ctx")
+    if status is None:
+        _refuse(what, "status is None")
+    return (kind, B, S, heads, kshape[2], dim, pq, sq[0], sq[1], sq[2], pk, sk[0], sk[1], sk[2], pv, sv[0], sv[1], sv[2],
+            pc, sc[0], sc[1], sc[2], pr, _table(what, "lse", lse, (B, heads, S), torch.float32, dev)), shape, kshape, dtype, dev
 
 
-def _attention_desc(what, q, k, v, ctx, lse, status, scale, cap, slopes, causal, prefix, docs, lens, rest) -> AttentionDesc:
-    import torch
-    _float_or_bf16(what, "q", q, 4)
-    B, S, heads, dim = q.shape
-    _same(what, q, (B, S, k.shape[2] if k.dim() == 4 else 0, dim), k=k, v=v)
-    _same(what, q, q.shape, ctx=ctx, rest=rest)
-    if rest is not None and rest.stride() != ctx.stride():
-        _refuse(what, "rest must have the strides of ctx")
-    _table(what, q, (B, heads, S), torch.float32, lse=lse)
-    _table(what, q, (heads,), torch.float32, slopes=slopes)
-    _table(what, q, (B,), torch.int32, prefix=prefix, lens=lens)
-    _table(what, q, (B, S), torch.int32, docs=docs)
-    _table(what, q, (1,), torch.int32, status=status)
-    d = AttentionDesc(_dt(q), B, S, heads, k.shape[2], dim, _heads(q), _heads(k), _heads(v), _heads(ctx), _ptr(rest), _ptr(lse))
-    d.scale, d.cap, d.causal = scale, cap, int(causal)
-    d.slopes, d.prefix, d.docs, d.lens = _ptr(slopes), _ptr(prefix), _ptr(docs), _ptr(lens)
-    return d
+def _mask_fields(what, shape, dev, scale, cap, slopes, causal, prefix, docs, lens):
+    i32 = _torch.int32
+    return (scale, cap, _table(what, "slopes", slopes, shape[2:3], _torch.float32, dev), bool(causal),
+            _table(what, "prefix", prefix, shape[:1], i32, dev), _table(what, "docs", docs, shape[:2], i32, dev),
+            _table(what, "lens", lens, shape[:1], i32, dev))
 
 
 def mslt_op_attention_masked(q, k, v, ctx, lse, scale: float, status, stream: int, cap: float = 0.0, slopes=None,
                              causal: bool = False, prefix=None, docs=None, lens=None, rest=None, sync: bool = True) -> None:
     """q, ctx [B, S, heads, head_dim], k, v [B, S, kv_heads, head_dim] float or bf16; lse fp32 [B, heads, S] or None;
     slopes fp32 [heads], prefix and lens int32 [B], docs int32 [B, S], rest bf16 like ctx: CUDA tensors or None."""
-    d = _attention_desc("attention_masked", q, k, v, ctx, lse, status, scale, cap, slopes, causal, prefix, docs, lens, rest)
-    _call(q, lib.mslt_op_attention_masked, C.byref(d), status.data_ptr(), stream, int(sync))
+    what = "attention_masked"
+    f, shape, _, _, dev = _attention_fields(what, q, k, v, ctx, lse, status, rest)
+    d = _ATTN.pack(*f, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0,
+                   *_mask_fields(what, shape, dev, scale, cap, slopes, causal, prefix, docs, lens))
+    _call(dev, lib.mslt_op_attention_masked, d, _table(what, "status", status, (1,), _torch.int32, dev), stream, sync)
 
 
 def mslt_op_attention_masked_bwd_scratch_bytes(B: int, S: int, heads: int) -> int:
@@ -482,15 +521,15 @@ def mslt_op_attention_masked_bwd(q, k, v, ctx, lse, dctx, dq, dk, dv, scratch, s
                                  sync: bool = True) -> None:
     """The other arguments as in mslt_op_attention_masked (ctx, lse and rest are its results); dctx, dq like q, dk, dv
     like k; scratch uint8."""
-    import torch
     what = "attention_masked_bwd"
-    d = _attention_desc(what, q, k, v, ctx, lse, status, scale, cap, slopes, causal, prefix, docs, lens, rest)
-    _same(what, q, q.shape, dctx=dctx, dq=dq)
-    _same(what, q, k.shape, dk=dk, dv=dv)
-    _table(what, q, scratch.shape, torch.uint8, scratch=scratch)
-    d.dctx, d.dq, d.dk, d.dv = _heads(dctx), _heads(dq), _heads(dk), _heads(dv)
-    _call(q, lib.mslt_op_attention_masked_bwd, C.byref(d), scratch.data_ptr(), scratch.numel(), status.data_ptr(), stream,
-          int(sync))
+    f, shape, kshape, dtype, dev = _attention_fields(what, q, k, v, ctx, lse, status, rest)
+    grads = ()
+    for name, t, sh in (("dctx", dctx, shape), ("dq", dq, shape), ("dk", dk, kshape), ("dv", dv, kshape)):
+        ptr, st = _view(what, name, t, sh, dtype, dev)
+        grads += (ptr, st[0], st[1], st[2])
+    d = _ATTN.pack(*f, *grads, *_mask_fields(what, shape, dev, scale, cap, slopes, causal, prefix, docs, lens))
+    _call(dev, lib.mslt_op_attention_masked_bwd, d, _table(what, "scratch", scratch, scratch.shape, _torch.uint8, dev), scratch.numel(),
+          _table(what, "status", status, (1,), _torch.int32, dev), stream, sync)
 
 
 class Mslt:

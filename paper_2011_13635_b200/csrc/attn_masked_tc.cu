@@ -25,7 +25,7 @@
 // them.
 #include <math.h>
 
-#include <atomic>
+#include <type_traits>
 
 #include "attn_masked.h"
 #include "tc_common.cuh"
@@ -36,7 +36,7 @@ bool attn_take_starve();  // whether the next attention launch was asked to run 
 namespace {
 
 constexpr int AM_ROWS = 128;      // rows of a block
-constexpr int AF_COLS = 64, AB_COLS = 128;  // rows of a loop block, forward and backward
+constexpr int AF_COLS = 64;       // rows of a loop block of the forward
 constexpr int AF_SOFT = 4, AF_THREADS = 64 + 32 * AF_SOFT;  // forward: softmax warps, threads
 constexpr int AB_SOFT = 16, AB_THREADS = 64 + 32 * AB_SOFT;  // backward
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -52,8 +52,10 @@ constexpr float AM_MOST = 1.2379400392853803e27f, AM_LEAST = 5.421010862427522e-
 struct View { bf16* p; long long batch, row, head; };
 struct TcParams {
   AttnMask m;
-  int heads, kv_heads, D, tiles;
+  int heads, kv_heads, D, tiles, batch;
+  int list_room;        // entries of a list of loop blocks
   View o0, o1;          // ctx | dq | dk, dv
+  int wide;             // rows of the outputs allow 32-byte stores
   bf16* rest;
   float* lse;
   const float* delta;
@@ -70,6 +72,11 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+__device__ __forceinline__ void tc_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -212,17 +219,77 @@ __device__ __forceinline__ int list_blocks(const AttnMask& m, const Seq& s, int 
   return red[8];
 }
 
+// The same by one warp, which runs ahead of the others: blocks of the persistent backward kernels.
+template <bool kKeys, int kCols>
+__device__ __forceinline__ int list_blocks_warp(const AttnMask& m, const Seq& s, int b, int r0, uint16_t* list) {
+  const int lane = threadIdx.x & 31;
+  const int* docs = m.docs ? m.docs + (long long)b * m.S : nullptr;
+  if (r0 >= s.len) return 0;
+  const int r1 = min(r0 + AM_ROWS, s.len) - 1;
+  auto range = [&](int c0, int rows, int (&d)[4], int* lo, int* hi) {  // of the documents of rows c0 + 32 e + lane
+    int mn = 0x7fffffff, mx = (int)0x80000000;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+      if (32 * e < rows && c0 + 32 * e + lane < s.len) {
+        mn = min(mn, d[e]);
+        mx = max(mx, d[e]);
+      }
+    *lo = __reduce_min_sync(0xffffffffu, mn);
+    *hi = __reduce_max_sync(0xffffffffu, mx);
+  };
+  auto ask = [&](int c0, int rows, int (&d)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      const int c = c0 + 32 * e + lane;
+      d[e] = 32 * e < rows && c < s.len ? docs[c] : 0;
+    }
+  };
+  int lo = 0, hi = 0;
+  if (docs) {
+    int d[4];
+    ask(r0, AM_ROWS, d);
+    range(r0, AM_ROWS, d, &lo, &hi);
+  }
+  const int first = kKeys && r0 >= s.prefix ? r0 / kCols : 0;
+  const int last = ((kKeys ? s.len : min(s.len, max(r1 + 1, s.prefix))) + kCols - 1) / kCols;
+  int n = 0;
+  constexpr int kAhead = 4;
+  for (int base = first; base < last; base += kAhead) {
+    int d[kAhead][4];
+    if (docs)
+#pragma unroll
+      for (int u = 0; u < kAhead; u++) ask((base + u) * kCols, kCols, d[u]);
+#pragma unroll
+    for (int u = 0; u < kAhead; u++) {
+      const int blk = base + u, c0 = blk * kCols;
+      if (blk >= last) break;
+      bool visit = true;
+      bool whole = c0 + kCols <= s.len && (kKeys ? (c0 >= r1 || r1 < s.prefix) : (c0 + kCols - 1 <= r0 || c0 + kCols <= s.prefix));
+      if (docs) {
+        int mn, mx;
+        range(c0, kCols, d[u], &mn, &mx);
+        visit = mn <= hi && mx >= lo;
+        whole = whole && lo == hi && mn == lo && mx == lo;
+      }
+      if (visit) {
+        if (lane == 0) list[n] = (uint16_t)(blk * 2 + !whole);
+        n++;
+      }
+    }
+  }
+  return n;
+}
+
 // Which of the 32 loop rows from c0 on row r counts a pair with; the whole warp.  The loop rows' documents lie one a lane;
 // the warp's own rows seldom hold more than two or three, and each of those takes one ballot for all rows that have it.
+// other: the document of loop row c0 + lane, asked for a step ahead.
 template <bool kKeys>
-__device__ __forceinline__ uint32_t visible(const Seq& s, int r, int c0, const int* docs, int doc) {
+__device__ __forceinline__ uint32_t visible(const Seq& s, int r, int c0, bool docs, int doc, int other) {
   const int end = (kKeys ? s.len : min(s.len, max(r + 1, s.prefix))) - c0;
   const int begin = (kKeys && r >= s.prefix ? r : 0) - c0;
   uint32_t w = end >= 32 ? 0xffffffffu : end <= 0 ? 0u : (1u << end) - 1;
   if (begin > 0) w = begin >= 32 ? 0u : w & ~((1u << begin) - 1);
   if (docs) {
-    const int c = c0 + (int)(threadIdx.x & 31);
-    const int other = c < s.len ? docs[c] : 0;
     uint32_t same = 0, todo = 0xffffffffu;
     while (todo) {
       const int v = __shfl_sync(0xffffffffu, doc, __ffs(todo) - 1);
@@ -241,25 +308,26 @@ __device__ __forceinline__ uint32_t visible(const Seq& s, int r, int c0, const i
 // capped (and perhaps biased).
 //
 // The cap, cap tanh(z / cap).  The hardware's tanh has an error of 2^-11 of the value: a probability off by 2 % at a score of
-// 50.  Where |z| <= 3/4 cap throughout a warp's piece, tanh(u) is u times a polynomial of degree 5 in u^2 (least greatest error
-// on u^2 <= 9/16, 2.7e-8 of the value), on the multiply-add pipe and with all constants folded in; beyond,
-// 1 - 2 / (1 + e^(2u)), two special functions on top of the exponential's one, absolute error 2e-7.
-struct Form { float sl2, slope2, cap2, inv_cap2, z_by, small, b[6]; };
+// 50.  Where |z| <= 3/8 cap throughout a warp's piece, as nearly always, tanh(u) is u times a polynomial of degree 3 in u^2
+// (least greatest error on u^2 <= 9/64, 5.8e-8 of the value), on the multiply-add pipe and with all constants folded in;
+// beyond, 1 - 2 / (1 + e^(2u)), two special functions on top of the exponential's one, absolute error 2e-7.  (Degree 5 up
+// to 3/4 cap: forward of 2 x 12 x 4096 keys 247 us.)
+struct Form { float sl2, slope2, cap2, inv_cap2, z_by, small, b[4]; };
 template <int kForm>
 __device__ __forceinline__ Form form_of(const AttnMask& m, int h) {
   Form f;
   f.sl2 = m.scale * LOG2E;
   f.slope2 = kForm >= 1 && m.slopes ? m.slopes[h] * LOG2E : 0.f;
   if (kForm == 2) {
-    constexpr float kT[6] = {0.999999973f, -0.333329788f, 0.133256886f, -0.0533584462f, 0.0196113117f, -0.00473641511f};
+    constexpr float kT[4] = {0.999999942f, -0.333319918f, 0.132848227f, -0.0482874447f};
     const float k = m.scale / m.cap;
     f.cap2 = m.cap * LOG2E;
     f.inv_cap2 = 1.f / f.cap2;
     f.z_by = k * (2.f * LOG2E);  // 2^(s z_by) = e^(2 z / cap)
-    f.small = 0.75f / fabsf(k);
+    f.small = 0.375f / fabsf(k);
     float by = f.cap2 * k;
 #pragma unroll
-    for (int i = 0; i < 6; i++) {
+    for (int i = 0; i < 4; i++) {
       f.b[i] = kT[i] * by;
       by *= k * k;
     }
@@ -316,9 +384,9 @@ __device__ __forceinline__ float2 exponents(const Form& f, const Piece& p, float
   if (Wy::CAP == 0) return __ffma2_rn(s, splat2(f.sl2), t);
   if (Wy::CAP == 1) {
     const float2 y = __fmul2_rn(s, s);
-    float2 q = splat2(f.b[5]);
+    float2 q = splat2(f.b[3]);
 #pragma unroll
-    for (int i = 4; i >= 0; i--) q = __ffma2_rn(q, y, splat2(f.b[i]));
+    for (int i = 2; i >= 0; i--) q = __ffma2_rn(q, y, splat2(f.b[i]));
     if (!kBend) return __ffma2_rn(s, q, t);
     const float2 v = __fmul2_rn(s, q), th = __fmul2_rn(v, splat2(f.inv_cap2));
     *bend = __ffma2_rn(make_float2(-th.x, -th.y), th, splat2(1.f));
@@ -348,14 +416,14 @@ __device__ __forceinline__ void product_ss(uint32_t d, uint32_t a, uint32_t a_kb
       tc_mma(d, ad, bd, idesc, kb + k > 0 ? 1u : 0u);
     }
 }
-// D (+)= A B over kRows rows of B, each of DP contiguous elements.  A lies in tensor memory, 32 of the contraction in 16
-// columns, the next 32 `a_step` columns on.
-template <int kRows>
+// D (+)= A B over kRows rows of B, each of DP contiguous elements.  A lies in tensor memory, 16 kRun of the contraction in
+// 8 kRun columns, the next ones `a_step` columns on.
+template <int kRows, int kRun>
 __device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint32_t a_step, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   const uint32_t hi = (uint32_t)(make_smem_desc(0, 16) >> 32), lo = (uint32_t)make_smem_desc(0, kRows * 128);
 #pragma unroll
   for (int k = 0; k < kRows / 16; k++)
-    tc_mma_ts(d, a + (k >> 1) * a_step + (k & 1) * 8, ((uint64_t)hi << 32) | (lo + addr16(b) + k * 128), idesc, accumulate | (k > 0));
+    tc_mma_ts(d, a + (k / kRun) * a_step + (k % kRun) * 8, ((uint64_t)hi << 32) | (lo + addr16(b) + k * 128), idesc, accumulate | (k > 0));
 }
 
 template <int DP>
@@ -385,10 +453,23 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, int from, int t) {
       reinterpret_cast<uint4*>(tile + kb * kRows * 128)[v] = make_uint4(0, 0, 0, 0);
 }
 
+// 16 elements to memory, or the first 8 of them; wide: 32-byte stores.  A lane's row is its own 128-byte line, and a store takes the
+// load/store unit a cycle a line, so half as many stores are half the time (16-byte ones: 1650 cycles a tile of dQ, 3900 of
+// dK and dV).
+__device__ __forceinline__ void store16(bf16* dst, const uint32_t (&h)[8], bool wide, bool both) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]),
+                 "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7])
+                 : "memory");
+  } else {
+    *reinterpret_cast<uint4*>(dst) = make_uint4(h[0], h[1], h[2], h[3]);
+    if (both) *reinterpret_cast<uint4*>(dst + 8) = make_uint4(h[4], h[5], h[6], h[7]);
+  }
+}
 // Columns [c0, c1) of a row of an accumulator, scaled, to bf16 in memory (from dst on), 16 at a time; optionally what the
 // rounding took off.  zero: zeros whatever the accumulator holds; have: there is one.
-__device__ __forceinline__ void store_row(uint32_t taddr, bf16* dst, bf16* rest, float f, bool zero, bool have, bool write, int c0, int c1,
-                                          int D) {
+__device__ __forceinline__ void store_row(uint32_t taddr, bf16* dst, bf16* rest, float f, bool zero, bool have, bool write, bool wide, int c0,
+                                          int c1, int D) {
 #pragma unroll 2
   for (int c = c0; c < c1; c += 16) {
     uint32_t r[16];
@@ -397,22 +478,17 @@ __device__ __forceinline__ void store_row(uint32_t taddr, bf16* dst, bf16* rest,
 #pragma unroll
       for (int e = 0; e < 16; e++) r[e] = 0;
     }
-    if (!write) continue;
+    if (!write || c >= D) continue;
+    uint32_t hi[8], lo[8];
 #pragma unroll
-    for (int v = 0; v < 16; v += 8) {
-      if (c + v >= D) break;
-      uint4 hi, lo;
-      uint32_t *h = reinterpret_cast<uint32_t*>(&hi), *l = reinterpret_cast<uint32_t*>(&lo);
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        const float x = __uint_as_float(r[v + 2 * e]) * f, y = __uint_as_float(r[v + 2 * e + 1]) * f;
-        h[e] = pack2(x, y);
-        const float2 b = bf162_to_f2(h[e]);
-        l[e] = pack2(x - b.x, y - b.y);
-      }
-      *reinterpret_cast<uint4*>(dst + c + v) = hi;
-      if (rest) *reinterpret_cast<uint4*>(rest + c + v) = lo;
+    for (int e = 0; e < 8; e++) {
+      const float x = __uint_as_float(r[2 * e]) * f, y = __uint_as_float(r[2 * e + 1]) * f;
+      hi[e] = pack2(x, y);
+      const float2 b = bf162_to_f2(hi[e]);
+      lo[e] = pack2(x - b.x, y - b.y);
     }
+    store16(dst + c, hi, wide && c + 16 <= D, c + 16 <= D);
+    if (rest) store16(rest + c, lo, wide && c + 16 <= D, c + 16 <= D);
   }
 }
 
@@ -554,8 +630,10 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   const uint32_t tmem = tmem_slot;
   pdl_begin();
 
-  const int idx = blockIdx.x % p.tiles, h = blockIdx.x / p.tiles % p.heads, b = blockIdx.x / p.tiles / p.heads;
-  const int tile = p.m.causal ? p.tiles - 1 - idx : idx;  // causal: the tiles with the most keys start first
+  // causal: the tiles with the most keys start first; else the tiles of a head side by side, which read the same rows
+  const int per = p.heads * p.batch, other = p.m.causal ? (int)blockIdx.x % per : (int)blockIdx.x / p.tiles;
+  const int h = other % p.heads, b = other / p.heads;
+  const int tile = p.m.causal ? p.tiles - 1 - (int)blockIdx.x / per : (int)blockIdx.x % p.tiles;
   const int hk = h / (p.heads / p.kv_heads), r0 = tile * AM_ROWS;
   const Seq s = sequence(p.m, b);
   const int n = list_blocks<false, AF_THREADS / 32, AF_COLS>(p.m, s, b, r0, list, red);
@@ -628,7 +706,7 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         fine = landed(vfull, j) && mbar_wait(smem_u32(&pready[j & 1]), j >> 1 & 1, abort_flag, p.status);
         if (!fine) break;
         tc_fence_after();
-        product_ts<AF_COLS>(tmem + Sh::O_COL, tmem + (j % SB) * 64, 16, smem_u32(Vs + st * Sh::KV_BYTES), id_o, j > j0);
+        product_ts<AF_COLS, 2>(tmem + Sh::O_COL, tmem + (j % SB) * 64, 16, smem_u32(Vs + st * Sh::KV_BYTES), id_o, j > j0);
         if (SB == 2) tc_commit(smem_u32(&odone[j & 1]));
         // one buffer: the probabilities lie in it until the product with V, issued before, has read them
         if (SB == 1 && j + 1 < j1) scores(j + 1);
@@ -642,14 +720,23 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
       top = settled || r >= s.len ? 0.f : -INFINITY;
       sum = exact = make_float2(0.f, 0.f);
       uint32_t seen = 0;
+      int others[2] = {0, 0};  // documents of the next step's keys
+      auto ask = [&](int entry) {
+        if (!docs || !(entry & 1)) return;
+        const int c = (entry >> 1) * AF_COLS + lane;
+        others[0] = c < s.len ? docs[c] : 0;
+        others[1] = c + 32 < s.len ? docs[c + 32] : 0;
+      };
+      ask(list[0]);
       for (int j = j0; j < j1; j++) {
         const int entry = list[j - j0], c0 = (entry >> 1) * AF_COLS;
         const bool test = entry & 1;
         uint32_t see[2] = {~0u, ~0u};
         if (test) {
-          see[0] = visible<false>(s, r, c0, docs, doc);
-          see[1] = visible<false>(s, r, c0 + 32, docs, doc);
+          see[0] = visible<false>(s, r, c0, docs != nullptr, doc, others[0]);
+          see[1] = visible<false>(s, r, c0 + 32, docs != nullptr, doc, others[1]);
         }
+        if (j + 1 < j1) ask(list[j + 1 - j0]);
         seen |= see[0] | see[1];
         if (!mbar_wait(smem_u32(&sfull[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
         tc_fence_after();
@@ -721,7 +808,8 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
     const float total = sum.x + sum.y;
     const bool empty = r >= s.len || !(total > 0.f);
     const long long at = b * p.o0.batch + r * p.o0.row + h * p.o0.head;
-    store_row(trow + Sh::O_COL, p.o0.p + at, p.rest ? p.rest + at : nullptr, empty ? 0.f : 1.f / total, empty, n > 0, r < p.m.S, 0, DP, p.D);
+    store_row(trow + Sh::O_COL, p.o0.p + at, p.rest ? p.rest + at : nullptr, empty ? 0.f : 1.f / total, empty, n > 0, r < p.m.S, p.wide, 0, DP,
+              p.D);
     if (p.lse && r < p.m.S)
       p.lse[((long long)b * p.heads + h) * p.m.S + r] = empty ? -INFINITY : (top + log2f(exact.x + exact.y)) * LN2;
   }
@@ -769,41 +857,52 @@ masked_delta_tc(const View dc, const View c, const bf16* rest, float* delta, int
   if (n < rows && e == 0) delta[(b * heads + h) * S + i] = sum;
 }
 
-// Tensor memory and stages of the two backward kernels: S 128 columns, dP 128, the accumulators DP or 2 DP.  S has a second
-// buffer, so that the next block's products run under this block's softmax, but for dK and dV of heads wider than 64, which
-// fill the 512 columns.
+// Tensor memory, loop blocks and stages of the two backward kernels.  Heads of 64: S 2 x 128 columns (the next block's
+// products run under this block's softmax), dP 128 (read at once, so the next one follows soon), the accumulators 64 or
+// 128.  Wider heads, dQ: the same with an accumulator of 128.  Wider heads, dK and dV: 256 columns of accumulators leave
+// 256, two blocks of 64 x (S, dP).  (One of 128 x (S, dP): products and softmax take turns, 2 x 12 x 4096 x 128 in 877 us.)
 template <int DP, bool kKeys> struct BwdShape {
-  static constexpr int SB = DP == 128 && kKeys ? 1 : 2;
-  static constexpr int STAGES = DP == 128 ? 2 : 4;
+  static constexpr int LOOP = DP == 128 && kKeys ? 64 : 128;      // rows of a loop block
+  static constexpr int SB = 2, PB = DP == 128 && kKeys ? 2 : 1;   // buffers of S, of dP
+  static constexpr int FB = DP == 64 ? 2 : 1;                     // buffers of the row tiles
+  static constexpr int STAGES = DP == 128 && !kKeys ? 2 : 4;
   static constexpr int COLS = 512;
-  static constexpr int DP_COL = SB * 128, ACC_COL = DP_COL + 128;
-  static constexpr int FIX_BYTES = AM_ROWS * DP * 2, LOOP_BYTES = AB_COLS * DP * 2;
-  static constexpr int SMEM = 2 * FIX_BYTES + STAGES * 2 * LOOP_BYTES;
+  static constexpr int DP_COL = SB * LOOP, ACC_COL = DP_COL + PB * LOOP;
+  static constexpr int PART = LOOP / 4;                           // columns of a softmax thread
+  static constexpr int FIX_BYTES = AM_ROWS * DP * 2, LOOP_BYTES = LOOP * DP * 2;
+  static constexpr int SMEM = FB * 2 * FIX_BYTES + STAGES * 2 * LOOP_BYTES;
 };
+static_assert(BwdShape<64, true>::ACC_COL + 2 * 64 <= 512 && BwdShape<128, false>::ACC_COL + 128 <= 512 &&
+              BwdShape<128, true>::ACC_COL + 2 * 128 <= 512, "tensor memory");
 
 // kKeys = false: rows are queries (A = q, B = k, C = dctx, D = v; loop over keys), the result is dq.
 // kKeys = true: rows are keys (A = k, B = q, C = v, D = dctx; loop over the queries of every head that shares them): dk, dv.
+// Persistent, a block an SM: row tiles in turn, steps counted on from tile to tile so that the barriers' phases go on.  The
+// producer warp works out a tile's list and asks for its rows while the tile before is under way; only the reading of
+// the accumulators lies between two tiles.  (A launch of a block a tile: 8 x 12 x 2048 in 6 documents 344 us.)
 template <int DP, bool kKeys, int kForm>
 __global__ void __launch_bounds__(AB_THREADS, 1)
 masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
               const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmD, const TcParams p) {
+  enum { I_LIST, I_LEN, I_PREFIX, I_ROW, I_HEAD, I_BATCH };  // entries of its list, length, prefix, first row, head, sequence
   typedef BwdShape<DP, kKeys> Sh;
-  constexpr int NS = Sh::STAGES;
+  constexpr int NS = Sh::STAGES, FB = Sh::FB, SB = Sh::SB, PB = Sh::PB, LOOP = Sh::LOOP, PART = Sh::PART;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* As = smem;
-  uint8_t* Cs = smem + Sh::FIX_BYTES;
-  uint8_t* Bs = Cs + Sh::FIX_BYTES;                 // stage: B then D
-  uint16_t* list = (uint16_t*)(Bs + NS * 2 * Sh::LOOP_BYTES);
-  __shared__ uint64_t fixfull, full[NS], empty[NS], sfull[2], ready[2], dpread, done;
+  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);  // row tiles: A then C
+  uint8_t* Bs = smem + FB * 2 * Sh::FIX_BYTES;                                  // stage: B then D
+  uint16_t* lists = (uint16_t*)(Bs + NS * 2 * Sh::LOOP_BYTES);                  // two
+  __shared__ uint64_t fixfull[FB], fixempty[FB], full[NS], empty[NS], sfull[2], ready[2], dpread, done, accfree, listfull[2], listempty[2];
   __shared__ uint32_t tmem_slot;
-  __shared__ int red[16];
-  __shared__ __align__(16) float cols_of[kKeys ? AB_SOFT : 1][2][32];   // kKeys: -lse (log2) and -delta of a warp's queries
+  __shared__ int info[2][8];                                                    // of a tile: see I_*
+  __shared__ __align__(16) float cols_of[kKeys ? AB_SOFT : 1][2][32];           // kKeys: -lse (log2) and -delta of a warp's queries
   __shared__ __align__(8) int flag_mem[4];
   volatile int* abort_flag = flag_mem + 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    mbar_init(smem_u32(&fixfull), 1);
+    for (int i = 0; i < FB; i++) {
+      mbar_init(smem_u32(&fixfull[i]), 1);
+      mbar_init(smem_u32(&fixempty[i]), 1);
+    }
     for (int i = 0; i < NS; i++) {
       mbar_init(smem_u32(&full[i]), 1);
       mbar_init(smem_u32(&empty[i]), 1);
@@ -811,9 +910,12 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     for (int i = 0; i < 2; i++) {
       mbar_init(smem_u32(&sfull[i]), 1);
       mbar_init(smem_u32(&ready[i]), AB_SOFT);
+      mbar_init(smem_u32(&listfull[i]), 1);
+      mbar_init(smem_u32(&listempty[i]), AB_SOFT + 1);
     }
     mbar_init(smem_u32(&dpread), AB_SOFT);
     mbar_init(smem_u32(&done), 1);
+    mbar_init(smem_u32(&accfree), AB_SOFT);
     *abort_flag = 0;
     *reinterpret_cast<volatile long long*>(abort_flag + 1) = p.wait_limit;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -831,207 +933,325 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   const uint32_t tmem = tmem_slot;
   pdl_begin();
 
-  const int row_heads = kKeys ? p.kv_heads : p.heads, group = p.heads / p.kv_heads;
-  const int idx = blockIdx.x % p.tiles, hr = blockIdx.x / p.tiles % row_heads, b = blockIdx.x / p.tiles / row_heads;
-  const int tile = p.m.causal && !kKeys ? p.tiles - 1 - idx : idx;  // causal: the tiles with the longest loops start first
-  const int r0 = tile * AM_ROWS;
-  const Seq s = sequence(p.m, b);
-  const int n_list = list_blocks<kKeys, AB_THREADS / 32, AB_COLS>(p.m, s, b, r0, list, red);
-  const int n = kKeys ? n_list * group : n_list;
-  // loop step j: its list entry and head
-  auto entry_of = [&](int j) { return (int)list[kKeys ? j % n_list : j]; };
-  auto head_of = [&](int j) { return kKeys ? hr * group + j / n_list : hr / group; };
+  const int row_heads = kKeys ? p.kv_heads : p.heads, group = p.heads / p.kv_heads, spans = kKeys ? group : 1;
+  const int items = p.tiles * row_heads * p.batch;
+  struct Item { int r0, hr, b; };
+  auto item_at = [&](int w) {
+    Item it;
+    if (p.m.causal) {  // the tiles with the longest loops first
+      const int per = row_heads * p.batch, t = w / per, x = w - t * per;
+      it.b = x / row_heads;
+      it.hr = x - it.b * row_heads;
+      it.r0 = (kKeys ? t : p.tiles - 1 - t) * AM_ROWS;
+    } else {           // tiles of a head side by side: they read the same rows
+      const int x = w / p.tiles;
+      it.r0 = (w - x * p.tiles) * AM_ROWS;
+      it.b = x / row_heads;
+      it.hr = x - it.b * row_heads;
+    }
+    return it;
+  };
 
-  if (warp == 0 && n > 0 && !p.starve && elect_one()) {
-    // ------------------------------- TMA producer -------------------------------
-    const uint32_t fb = smem_u32(&fixfull);
-    mbar_expect_tx(fb, 2 * Sh::FIX_BYTES);
-    load_rows<DP>(smem_u32(As), &tmA, p.a_perm, fb, r0, hr, b, 16384);
-    load_rows<DP>(smem_u32(Cs), &tmC, p.c_perm, fb, r0, hr, b, 16384);
-    int issued = 0;
-    for (int j = 0; j < n; j++) {
-      const int st = j % NS, row = (entry_of(j) >> 1) * AB_COLS, hl = head_of(j);
-      if (!mbar_wait(smem_u32(&empty[st]), (uint32_t)(j / NS & 1) ^ 1, abort_flag, p.status)) break;
-      const uint32_t bar = smem_u32(&full[st]), dst = smem_u32(Bs + st * 2 * Sh::LOOP_BYTES);
-      mbar_expect_tx(bar, 2 * Sh::LOOP_BYTES);
-      load_rows<DP>(dst, &tmB, p.b_perm, bar, row, hl, b, 16384);
-      load_rows<DP>(dst + Sh::LOOP_BYTES, &tmD, p.d_perm, bar, row, hl, b, 16384);
-      issued = j + 1;
+  if (warp == 0 && !p.starve) {
+    // ------------------------------- producer -------------------------------
+    int g = 0, tiles_done = 0, i = 0;  // steps and tiles so far
+    bool ok = true;
+    for (int w = blockIdx.x; w < items; w += gridDim.x, i++) {
+      const Item it = item_at(w);
+      const int slot = i & 1;
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&listempty[slot]), (uint32_t)(i >> 1 & 1) ^ 1, abort_flag, p.status));
+      int n_list = 0;
+      uint16_t* list = lists + slot * p.list_room;
+      if (ok) {
+        const Seq s = sequence(p.m, it.b);
+        n_list = list_blocks_warp<kKeys, LOOP>(p.m, s, it.b, it.r0, list);
+        if (lane == 0) {
+          info[slot][I_LIST] = n_list;
+          info[slot][I_LEN] = s.len;
+          info[slot][I_PREFIX] = s.prefix;
+          info[slot][I_ROW] = it.r0;
+          info[slot][I_HEAD] = it.hr;
+          info[slot][I_BATCH] = it.b;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&listfull[slot]));
+      }
+      const int n = n_list * spans;
+      if (ok && n == 0) continue;
+      if (elect_one()) {
+        const int f = tiles_done % FB;
+        int issued = g, fixed = tiles_done;  // steps and row tiles asked for
+        const uint32_t fb = smem_u32(&fixfull[f]), fix = smem_u32(smem + f * 2 * Sh::FIX_BYTES);
+        ok = ok && mbar_wait(smem_u32(&fixempty[f]), (uint32_t)(tiles_done / FB & 1) ^ 1, abort_flag, p.status);
+        if (ok) {
+          mbar_expect_tx(fb, 2 * Sh::FIX_BYTES);
+          load_rows<DP>(fix, &tmA, p.a_perm, fb, it.r0, it.hr, it.b, 16384);
+          load_rows<DP>(fix + Sh::FIX_BYTES, &tmC, p.c_perm, fb, it.r0, it.hr, it.b, 16384);
+          fixed = tiles_done + 1;
+        }
+        int at_list = 0, hl = kKeys ? it.hr * group : it.hr / group;
+        for (int j = g; j < g + n && ok; j++) {
+          const int st = j % NS, row = (list[at_list] >> 1) * LOOP;
+          ok = mbar_wait(smem_u32(&empty[st]), (uint32_t)(j / NS & 1) ^ 1, abort_flag, p.status);
+          if (!ok) break;
+          const uint32_t bar = smem_u32(&full[st]), dst = smem_u32(Bs + st * 2 * Sh::LOOP_BYTES);
+          mbar_expect_tx(bar, 2 * Sh::LOOP_BYTES);
+          load_rows<DP>(dst, &tmB, p.b_perm, bar, row, hl, it.b, LOOP * 128);
+          load_rows<DP>(dst + Sh::LOOP_BYTES, &tmD, p.d_perm, bar, row, hl, it.b, LOOP * 128);
+          issued = j + 1;
+          if (++at_list == n_list) {
+            at_list = 0;
+            hl++;
+          }
+        }
+        if (!ok || *abort_flag) {
+          // what has been asked for must have landed before the block leaves
+          for (int t = max(0, fixed - FB); t < fixed; t++) drain(&fixfull[t % FB], (t / FB) & 1);
+          for (int j = max(0, issued - NS); j < issued; j++) drain(&full[j % NS], (j / NS) & 1);
+          ok = false;
+        }
+      }
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      g += n;
+      tiles_done++;
     }
-    if (issued < n || *abort_flag) {
-      drain(&fixfull, 0);
-      for (int j = max(0, issued - NS); j < issued; j++) drain(&full[j % NS], (j / NS) & 1);
-    }
-  } else if (warp == 1 && n > 0 && elect_one()) {
+  } else if (warp == 1 && elect_one()) {
     // ------------------------------- products -------------------------------
-    constexpr uint32_t id_s = idesc_of(AB_COLS, false), id_acc = idesc_of(DP, true);
+    constexpr uint32_t id_s = idesc_of(LOOP, false), id_acc = idesc_of(DP, true);
     auto stage = [&](int j) { return smem_u32(Bs + (j % NS) * 2 * Sh::LOOP_BYTES); };
-    auto landed = [&](int j) {
-      if (!mbar_wait(smem_u32(&full[j % NS]), j / NS & 1, abort_flag, p.status)) return false;
-      tc_fence_after();
-      return true;
-    };
-    auto scores = [&](int j) { product_ss<DP>(tmem + (j % Sh::SB) * 128, smem_u32(As), 1024, stage(j), 1024, id_s); };
-    auto dprobs = [&](int j) {
-      product_ss<DP>(tmem + Sh::DP_COL, smem_u32(Cs), 1024, stage(j) + Sh::LOOP_BYTES, 1024, id_s);
-    };
-    bool ok = mbar_wait(smem_u32(&fixfull), 0, abort_flag, p.status) && landed(0);
-    if (ok) {
-      scores(0);
-      dprobs(0);
-      tc_commit(smem_u32(&sfull[0]));
-    }
-    for (int j = 0; j < n && ok; j++) {
-      const bool more = j + 1 < n;
-      if (more) {
-        if (!landed(j + 1)) { ok = false; break; }
-        if (Sh::SB == 2) scores(j + 1);
-        if (!mbar_wait(smem_u32(&dpread), j & 1, abort_flag, p.status)) { ok = false; break; }
+    auto landed = [&](int j) { return mbar_wait(smem_u32(&full[j % NS]), j / NS & 1, abort_flag, p.status); };
+    int g = 0, tiles_done = 0, i = 0;
+    bool ok = true;
+    for (int w = blockIdx.x; w < items && ok; w += gridDim.x, i++) {
+      const int slot = i & 1;
+      if (!mbar_wait(smem_u32(&listfull[slot]), i >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
+      const int n = info[slot][I_LIST] * spans;
+      mbar_arrive(smem_u32(&listempty[slot]));
+      if (n == 0) continue;
+      const int f = tiles_done % FB;
+      const uint32_t fix = smem_u32(smem + f * 2 * Sh::FIX_BYTES);
+      auto scores = [&](int j) { product_ss<DP>(tmem + (j % SB) * LOOP, fix, 1024, stage(j), LOOP * 8, id_s); };
+      auto dprobs = [&](int j) {
+        product_ss<DP>(tmem + Sh::DP_COL + (j % PB) * LOOP, fix + Sh::FIX_BYTES, 1024, stage(j) + Sh::LOOP_BYTES, LOOP * 8, id_s);
+      };
+      // S and dP of step j.  Their buffers: what lay in the scores' was last read by a product issued before; dP, where it has
+      // one, by the softmax of the step before.
+      auto next = [&](int j) {
+        if (!landed(j)) return false;
         tc_fence_after();
-        dprobs(j + 1);
-        if (Sh::SB == 2) tc_commit(smem_u32(&sfull[(j + 1) & 1]));
+        scores(j);
+        if (PB == 1 && j > 0) {
+          if (!mbar_wait(smem_u32(&dpread), (j - 1) & 1, abort_flag, p.status)) return false;
+          tc_fence_after();
+        }
+        dprobs(j);
+        tc_commit(smem_u32(&sfull[j & 1]));
+        return true;
+      };
+      ok = mbar_wait(smem_u32(&fixfull[f]), tiles_done / FB & 1, abort_flag, p.status) && next(g);
+      for (int j = g; j < g + n && ok; j++) {
+        if (j + 1 < g + n) {
+          if (!next(j + 1)) { ok = false; break; }
+        } else {
+          tc_commit(smem_u32(&fixempty[f]));
+        }
+        if (!mbar_wait(smem_u32(&ready[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
+        if (j == g && tiles_done > 0 && !mbar_wait(smem_u32(&accfree), (tiles_done - 1) & 1, abort_flag, p.status)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t at = tmem + (j % SB) * LOOP;
+        if (kKeys) {
+          product_ts<LOOP, 1>(tmem + Sh::ACC_COL, at, 16, stage(j) + Sh::LOOP_BYTES, id_acc, j > g);    // dV += P^T dC
+          product_ts<LOOP, 1>(tmem + Sh::ACC_COL + DP, at + 8, 16, stage(j), id_acc, j > g);            // dK += dS^T Q
+        } else {
+          product_ts<LOOP, 1>(tmem + Sh::ACC_COL, at, 16, stage(j), id_acc, j > g);                     // dQ += dS K
+        }
+        tc_commit(smem_u32(&empty[j % NS]));
       }
-      if (!mbar_wait(smem_u32(&ready[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
-      tc_fence_after();
-      const uint32_t at = tmem + (j % Sh::SB) * 128;
-      if (kKeys) {
-        product_ts<AB_COLS>(tmem + Sh::ACC_COL, at, 32, stage(j) + Sh::LOOP_BYTES, id_acc, j > 0);    // dV += P^T dC
-        product_ts<AB_COLS>(tmem + Sh::ACC_COL + DP, at + 16, 32, stage(j), id_acc, j > 0);           // dK += dS^T Q
-      } else {
-        product_ts<AB_COLS>(tmem + Sh::ACC_COL, at, 32, stage(j), id_acc, j > 0);                     // dQ += dS K
-      }
-      if (more && Sh::SB == 1) {
-        scores(j + 1);
-        tc_commit(smem_u32(&sfull[(j + 1) & 1]));
-      }
-      tc_commit(smem_u32(&empty[j % NS]));
+      if (!ok) break;
+      tc_commit(smem_u32(&done));
+      g += n;
+      tiles_done++;
     }
-    if (ok) tc_commit(smem_u32(&done));
     if (!ok || *abort_flag) settle(&done);
   } else if (warp >= 2) {
-    // ------------------ softmax and its backward: a thread owns 32 columns of a row ------------------
-    const int quarter = warp & 3, part = (warp - 2) >> 2, r = r0 + quarter * 32 + lane;
-    const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16) + part * 32;
-    const int* docs = p.m.docs ? p.m.docs + (long long)b * p.m.S : nullptr;
-    const int doc = docs && r < s.len ? docs[r] : 0;
-    Form f = form_of<kForm>(p.m, kKeys ? hr * group : hr);
-    // lse and delta: of the row (queries), or of the lane's column of the next step (keys).  Those are asked for a step ahead and
-    // not touched before they are needed (multiplied where they were asked for, they cost 1000 of 2700 cycles a step).
+    // ------------------ softmax and its backward: a thread owns PART columns of a row ------------------
+    const int quarter = warp & 3, part = (warp - 2) >> 2;
+    const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16) + part * PART;
+    int g = 0, tiles_done = 0, i = 0;
+    bool ok = true;
+    // What the common step does not need stays in shared memory: registers are short.
+    const volatile int* it = info[0];
+    // lse and delta of the row (queries), or of the lane's column of the next step (keys), and documents of the row and of the
+    // next step's columns.  They are asked for ahead and not touched before they are needed (multiplied where they were asked
+    // for, they cost 1000 of 2700 cycles a step): a step ahead, and a tile's first ones before the tile before is stored.
     float lse = 0.f, delta = 0.f;
-    auto ask = [&](int h, int i) {
-      const long long at = ((long long)b * p.heads + h) * p.m.S + i;
+    int doc = 0, other = 0;
+    auto ask = [&](int h, int c) {
+      const long long at = ((long long)it[I_BATCH] * p.heads + h) * p.m.S + c;
       lse = delta = 0.f;
-      if (i < s.len) {
+      if (c < it[I_LEN]) {
         lse = p.lse[at];
         delta = p.delta[at];
       }
     };
-    if (!kKeys) ask(hr, r);
-    else if (n > 0) ask(hr * group, (list[0] >> 1) * AB_COLS + part * 32 + lane);
-    const float lse2 = lse * LOG2E;
-    int at_list = 0, head = kKeys ? hr * group : hr / group;  // of step j
-    bool ok = true;
-    for (int j = 0; j < n; j++) {
-      const int entry = list[at_list], c0 = (entry >> 1) * AB_COLS + part * 32;
-      const bool test = entry & 1;
-      if (kKeys) {
-        __syncwarp();
-        cols_of[warp - 2][0][lane] = -lse * LOG2E;
-        cols_of[warp - 2][1][lane] = -delta;
-        __syncwarp();
-        if (kForm == 1 || kForm == 2) f.slope2 = p.m.slopes ? p.m.slopes[head] * LOG2E : 0.f;
-      }
-      if (++at_list == n_list) {
-        at_list = 0;
-        head++;
-      }
-      if (kKeys && j + 1 < n) ask(head, (list[at_list] >> 1) * AB_COLS + part * 32 + lane);
-      uint32_t see = ~0u;
-      if (test) see = visible<kKeys>(s, r, c0, docs, doc);
-      if (!mbar_wait(smem_u32(&sfull[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
-      tc_fence_after();
-      const uint32_t tS = trow + (j % Sh::SB) * 128, tP = trow + Sh::DP_COL;
-      uint32_t pp[16], ds[16];
+    auto ask_step = [&](int head, int entry) {
+      const int c = (entry >> 1) * LOOP + part * PART + lane;
+      if (kKeys && lane < PART) ask(head, c);
+      if ((entry & 1) && p.m.docs) other = c < it[I_LEN] ? p.m.docs[(long long)it[I_BATCH] * p.m.S + c] : 0;
+    };
+    auto enter = [&](int tile) {  // the block's tile-th tile
+      if (!mbar_wait(smem_u32(&listfull[tile & 1]), tile >> 1 & 1, abort_flag, p.status)) return false;
+      it = info[tile & 1];
+      const int r = it[I_ROW] + quarter * 32 + lane;
+      if (!kKeys) ask(it[I_HEAD], r);
+      if (p.m.docs) doc = r < it[I_LEN] ? p.m.docs[(long long)it[I_BATCH] * p.m.S + r] : 0;
+      if (it[I_LIST] > 0) ask_step(kKeys ? it[I_HEAD] * group : 0, lists[(tile & 1) * p.list_room]);
+      return true;
+    };
+    if ((int)blockIdx.x < items) ok = enter(0);
+    for (int w = blockIdx.x; w < items && ok; w += gridDim.x, i++) {
+      const int slot = i & 1;
+      const int n_list = it[I_LIST], n = n_list * spans, r = it[I_ROW] + quarter * 32 + lane;
+      const uint16_t* list = lists + slot * p.list_room;
+      Form f = form_of<kForm>(p.m, it[I_HEAD] * spans);
+      int at_list = 0, head = kKeys ? it[I_HEAD] * group : it[I_HEAD] / group;  // of step j
+      const float lse2 = lse * LOG2E;
+      for (int j = g; j < g + n; j++) {
+        const int entry = list[at_list], first = (entry >> 1) * LOOP, c0 = first + part * PART;
+        const bool test = entry & 1;
+        if (kKeys) {
+          __syncwarp();
+          cols_of[warp - 2][0][lane] = -lse * LOG2E;
+          cols_of[warp - 2][1][lane] = -delta;
+          __syncwarp();
+          if (kForm == 1 || kForm == 2) f.slope2 = p.m.slopes ? p.m.slopes[head] * LOG2E : 0.f;
+        }
+        uint32_t see = ~0u;
+        if (test) {
+          Seq s;
+          s.len = it[I_LEN];
+          s.prefix = it[I_PREFIX];
+          see = visible<kKeys>(s, r, c0, p.m.docs != nullptr, doc, other);
+        }
+        if (++at_list == n_list) {
+          at_list = 0;
+          head++;
+        }
+        if (j + 1 < g + n) ask_step(head, list[at_list]);
+        if (!mbar_wait(smem_u32(&sfull[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t tS = trow + (j % SB) * LOOP, tP = trow + Sh::DP_COL + (j % PB) * LOOP;
+        const bool tail = test && it[I_LEN] < first + LOOP;
 #pragma unroll
-      for (int q = 0; q < 32; q += 16) {  // 16 columns at a time: 32 need more than the 96 registers that 576 threads have
-      uint32_t a[16], d[16];
-      tc_ld16_issue(tS + q, a);
-      tc_ld16_issue(tP + q, d);
-      tc_ld16_wait(a);
-      tc_ld16_wait(d);
-      if (q) {
+        for (int q = 0; q < PART; q += 16) {    // 16 columns at a time: 32 need more than the 96 registers that 576 threads have
+          uint32_t out[kKeys ? 16 : 8];         // keys: P, then dS; queries: dS
+          uint32_t a[16], d[16];
+          tc_ld16_issue(tS + q, a);
+          tc_ld16_issue(tP + q, d);
+          tc_ld16_wait(a);
+          tc_ld16_wait(d);
+          auto read = [&] {
+            if (PB == 1 && q + 16 == PART) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(smem_u32(&dpread));
+            }
+          };
+          if (!test) read();
+          const Piece pc = piece_of<kForm>(f, r, c0 + q, a);
+          const uint32_t seen = see >> q;
+          float most = 0.f;
+          auto gradients = [&](bool tested, auto careful) {
+            choose_way<kForm>(f, pc, tested, [&](auto way) {
+              typedef decltype(way) Wy;
+              float4 nl4, nd4;
+#pragma unroll
+              for (int c = 0; c < 16; c += 2) {
+                float2 x = make_float2(__uint_as_float(a[c]), __uint_as_float(a[c + 1]));
+                float2 t = make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
+                float2 nl = splat2(-lse2), nd = splat2(-delta), bend = splat2(1.f);
+                if (kKeys) {
+                  if (c % 4 == 0) {
+                    nl4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][0][q + c]);
+                    nd4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][1][q + c]);
+                  }
+                  nl = c % 4 ? make_float2(nl4.z, nl4.w) : make_float2(nl4.x, nl4.y);
+                  nd = c % 4 ? make_float2(nd4.z, nd4.w) : make_float2(nd4.x, nd4.y);
+                }
+                x = exponents<Wy, true>(f, pc, x, c, nl, &bend);
+                const bool v0 = !Wy::TEST || (seen >> c & 1), v1 = !Wy::TEST || (seen >> (c + 1) & 1);
+                x.x = ex2(v0 ? x.x : -INFINITY);
+                x.y = ex2(v1 ? x.y : -INFINITY);
+                t = __fmul2_rn(__fadd2_rn(t, nd), x);
+                if (Wy::CAP) t = __fmul2_rn(t, bend);
+                if (Wy::TEST && !decltype(careful)::value) most = fmaxf(most, fmaxf(x.x, x.y));
+                if (decltype(careful)::value) {
+                  t.x = v0 && !(x.x > 0.99999f) ? t.x : 0.f;
+                  t.y = v1 && !(x.y > 0.99999f) ? t.y : 0.f;
+                }
+                if (kKeys) out[c / 2] = pack2(x.x, x.y);
+                out[(kKeys ? 8 : 0) + c / 2] = pack2(t.x, t.y);
+              }
+            });
+          };
+          if (!tail) gradients(test, std::false_type());
+          // Two rare cases are looked at pair by pair.  Columns beyond the sequence, whose dP may be anything.  And a row with a
+          // single key, which has no gradient by its score: dP - delta is the difference of two sums in different orders there,
+          // and is zero in truth.  p(dP_j - delta) is at most (1 - p) times the spread of dP, so nothing above 1e-5 of it
+          // is dropped; a block without pairs to test has as many keys a row as columns, and no such p alone.
+          if (tail || (test && __any_sync(0xffffffffu, most > 0.99999f))) {
+            if (!tail) {  // the first time used them up
+              tc_ld16_issue(tS + q, a);
+              tc_ld16_issue(tP + q, d);
+              tc_ld16_wait(a);
+              tc_ld16_wait(d);
+            }
+            gradients(true, std::true_type());
+          }
+          if (test) read();
+          // over the scores that were just read
+          if constexpr (kKeys) tc_st16(tS + q, out);
+          else tc_st8(tS + q, out);
+        }
+        tc_st_wait();
+        if (test && it[I_LEN] < first + LOOP) {
+          // the products' reads of this stage so far are over (S and dP are complete); its rows are an operand once more
+          uint8_t* tiles = Bs + (j % NS) * 2 * Sh::LOOP_BYTES;
+          clear_rows<DP, LOOP, 32 * AB_SOFT>(tiles, it[I_LEN] - first, threadIdx.x - 64);
+          if (kKeys) clear_rows<DP, LOOP, 32 * AB_SOFT>(tiles + Sh::LOOP_BYTES, it[I_LEN] - first, threadIdx.x - 64);
+          fence_proxy_async_smem();
+        }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&dpread));
+        if (lane == 0) mbar_arrive(smem_u32(&ready[j & 1]));
       }
-      const Piece pc = piece_of<kForm>(f, r, c0 + q, a);
-      const uint32_t seen = see >> q;
-      choose_way<kForm>(f, pc, test, [&](auto way) {
-        typedef decltype(way) Wy;
-        float4 nl4, nd4;
-#pragma unroll
-        for (int c = 0; c < 16; c += 2) {
-          float2 x = make_float2(__uint_as_float(a[c]), __uint_as_float(a[c + 1]));
-          float2 t = make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
-          float2 nl = splat2(-lse2), nd = splat2(-delta), bend = splat2(1.f);
-          if (kKeys) {
-            if (c % 4 == 0) {
-              nl4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][0][q + c]);
-              nd4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][1][q + c]);
-            }
-            nl = c % 4 ? make_float2(nl4.z, nl4.w) : make_float2(nl4.x, nl4.y);
-            nd = c % 4 ? make_float2(nd4.z, nd4.w) : make_float2(nd4.x, nd4.y);
-          }
-          x = exponents<Wy, true>(f, pc, x, c, nl, &bend);
-          x.x = ex2(x.x);
-          x.y = ex2(x.y);
-          t = __fmul2_rn(__fadd2_rn(t, nd), x);
-          if (Wy::CAP) t = __fmul2_rn(t, bend);
-          if (Wy::TEST) {
-            // A row with a single key has no gradient by its score: dP - delta is the difference of two sums in different
-            // orders there, and is zero in truth.  p(dP_j - delta) is at most (1 - p) times the spread of dP, so nothing
-            // above 1e-5 of it is dropped; a block without pairs to test has 64 keys a row and no such p alone.
-            const bool one0 = x.x > 0.99999f, one1 = x.y > 0.99999f;
-            const bool v0 = seen >> c & 1, v1 = seen >> (c + 1) & 1;
-            x.x = v0 ? x.x : 0.f;
-            x.y = v1 ? x.y : 0.f;
-            t.x = v0 && !one0 ? t.x : 0.f;
-            t.y = v1 && !one1 ? t.y : 0.f;
-          }
-          if (kKeys) pp[(q + c) / 2] = pack2(x.x, x.y);
-          ds[(q + c) / 2] = pack2(t.x, t.y);
-        }
-      });
-      }
-      // over the scores that this warp has read: keys, P and then dS; queries, dS
-      if (kKeys) tc_st16(tS, pp);
-      tc_st16(kKeys ? tS + 16 : tS, ds);
-      tc_st_wait();
-      const int first = (entry >> 1) * AB_COLS;
-      if (test && s.len < first + AB_COLS) {
-        // the products' reads of this stage so far are over (S and dP are complete); its rows are an operand once more
-        uint8_t* tiles = Bs + (j % NS) * 2 * Sh::LOOP_BYTES;
-        clear_rows<DP, AB_COLS, 32 * AB_SOFT>(tiles, s.len - first, threadIdx.x - 64);
-        if (kKeys) clear_rows<DP, AB_COLS, 32 * AB_SOFT>(tiles + Sh::LOOP_BYTES, s.len - first, threadIdx.x - 64);
-        fence_proxy_async_smem();
-      }
-      tc_fence_before();
+      if (!ok) break;
+      const int b = it[I_BATCH], hr = it[I_HEAD];
+      const bool dead = r >= it[I_LEN], write = r < p.m.S;
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&ready[j & 1]));
-    }
-    if (ok && n > 0) ok = mbar_wait(smem_u32(&done), 0, abort_flag, p.status);
-    if (ok) {
-      tc_fence_after();
-      const bool dead = r >= s.len, write = r < p.m.S;
+      if (lane == 0) mbar_arrive(smem_u32(&listempty[slot]));
+      if (w + (int)gridDim.x < items && !enter(i + 1)) { ok = false; break; }
+      if (n > 0) {
+        if (!mbar_wait(smem_u32(&done), tiles_done & 1, abort_flag, p.status)) { ok = false; break; }
+        tc_fence_after();
+      }
       const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16) + Sh::ACC_COL;
       if (kKeys) {
         const int which = part >> 1;  // 0: dV, 1: dK
         const View& o = which ? p.o0 : p.o1;
         store_row(acc + which * DP, o.p + (b * o.batch + r * o.row + hr * o.head), nullptr, which ? p.m.scale : 1.f, dead, n > 0, write,
-                  (part & 1) * (DP / 2), ((part & 1) + 1) * (DP / 2), p.D);
+                  p.wide, (part & 1) * (DP / 2), ((part & 1) + 1) * (DP / 2), p.D);
       } else {
-        store_row(acc, p.o0.p + (b * p.o0.batch + r * p.o0.row + hr * p.o0.head), nullptr, p.m.scale, dead, n > 0, write, part * (DP / 4),
-                  (part + 1) * (DP / 4), p.D);
+        store_row(acc, p.o0.p + (b * p.o0.batch + r * p.o0.row + hr * p.o0.head), nullptr, p.m.scale, dead, n > 0, write, p.wide,
+                  part * (DP / 4), (part + 1) * (DP / 4), p.D);
+      }
+      if (n > 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&accfree));
+        g += n;
+        tiles_done++;
       }
     }
   }
@@ -1069,6 +1289,8 @@ int map_of(const mslt_heads& h, const mslt_attention_desc& d, int heads, int box
   for (int i = 0; i < 3; i++) perm[i] = m->perm[i];
   return rc;
 }
+// whether every head's row starts on 32 bytes
+bool aligned32(const mslt_heads& h) { return ((uintptr_t)h.data & 31) == 0 && h.batch % 16 == 0 && h.row % 16 == 0 && h.head % 16 == 0; }
 View view_of(const mslt_heads& h) { return View{(bf16*)h.data, h.batch, h.row, h.head}; }
 
 TcParams params_of(const mslt_attention_desc& d, int* status, bool starve) {
@@ -1077,6 +1299,8 @@ TcParams params_of(const mslt_attention_desc& d, int* status, bool starve) {
   p.m = AttnMask{d.S, d.causal != 0, d.scale, d.cap, d.slopes, d.prefix, d.docs, d.lens};
   p.heads = d.heads; p.kv_heads = d.kv_heads; p.D = d.head_dim;
   p.tiles = (d.S + AM_ROWS - 1) / AM_ROWS;
+  p.batch = d.B;
+  p.list_room = (d.S + AF_COLS - 1) / AF_COLS;
   p.rest = (bf16*)d.rest; p.lse = d.lse;
   p.wait_limit = starve ? 40000000ll : WAIT_LIMIT_CYCLES;  // starved: about 20 ms
   p.starve = starve;
@@ -1097,22 +1321,23 @@ int forward(const mslt_attention_desc& d, TcParams& p, const MapVal* m, cudaStre
   return 0;
 }
 template <int DP, bool kKeys, int kForm>
-int backward(const mslt_attention_desc& d, TcParams& p, const MapVal* m, cudaStream_t st, char* err) {
+int backward(const mslt_attention_desc& d, TcParams& p, const MapVal* m, int sms, cudaStream_t st, char* err) {
   static bool done[kMaxDevices];
   typedef BwdShape<DP, kKeys> Sh;
-  if (opt_in(masked_bwd_tc<DP, kKeys, kForm>, done, Sh::SMEM + kMostList, err)) return MSLT_ERR_CUDA;
-  launch_pdl(masked_bwd_tc<DP, kKeys, kForm>, d.B * (kKeys ? d.kv_heads : d.heads) * p.tiles, AB_THREADS, Sh::SMEM + list_bytes(d.S), st,
+  if (opt_in(masked_bwd_tc<DP, kKeys, kForm>, done, Sh::SMEM + 2 * kMostList, err)) return MSLT_ERR_CUDA;
+  const int items = d.B * (kKeys ? d.kv_heads : d.heads) * p.tiles;
+  launch_pdl(masked_bwd_tc<DP, kKeys, kForm>, items < sms ? items : sms, AB_THREADS, Sh::SMEM + 2 * list_bytes(d.S), st,
              m[0].map, m[1].map, m[2].map, m[3].map, p);
   return 0;
 }
 template <bool kKeys>
-int backward_of(const mslt_attention_desc& d, TcParams& p, const MapVal* m, cudaStream_t st, char* err) {
+int backward_of(const mslt_attention_desc& d, TcParams& p, const MapVal* m, int sms, cudaStream_t st, char* err) {
   const int form = form_index(d);
   if (d.head_dim <= 64)
-    return form == 0 ? backward<64, kKeys, 0>(d, p, m, st, err) : form == 1 ? backward<64, kKeys, 1>(d, p, m, st, err)
-                                                                            : backward<64, kKeys, 2>(d, p, m, st, err);
-  return form == 0 ? backward<128, kKeys, 0>(d, p, m, st, err) : form == 1 ? backward<128, kKeys, 1>(d, p, m, st, err)
-                                                                           : backward<128, kKeys, 2>(d, p, m, st, err);
+    return form == 0 ? backward<64, kKeys, 0>(d, p, m, sms, st, err) : form == 1 ? backward<64, kKeys, 1>(d, p, m, sms, st, err)
+                                                                            : backward<64, kKeys, 2>(d, p, m, sms, st, err);
+  return form == 0 ? backward<128, kKeys, 0>(d, p, m, sms, st, err) : form == 1 ? backward<128, kKeys, 1>(d, p, m, sms, st, err)
+                                                                           : backward<128, kKeys, 2>(d, p, m, sms, st, err);
 }
 
 }  // namespace
@@ -1125,6 +1350,7 @@ int attn_masked_tc_fwd(const mslt_attention_desc& d, int* status, cudaStream_t s
   if (!rc) rc = map_of(d.v, d, d.kv_heads, AF_COLS, &m[2], p.c_perm, err);
   if (rc) return rc;
   p.o0 = view_of(d.ctx);
+  p.wide = aligned32(d.ctx) && ((uintptr_t)d.rest & 31) == 0;
   const int form = form_index(d);
   if (d.head_dim <= 64)
     return form == 0 ? forward<64, 0>(d, p, m, st, err) : form == 1 ? forward<64, 1>(d, p, m, st, err) : forward<64, 2>(d, p, m, st, err);
@@ -1134,15 +1360,21 @@ int attn_masked_tc_fwd(const mslt_attention_desc& d, int* status, cudaStream_t s
 int attn_masked_tc_bwd(const mslt_attention_desc& d, float* delta, int* status, cudaStream_t st, char* err) {
   TcParams p = params_of(d, status, attn_take_starve());
   MapVal mq[4], mk[4];
+  const int loop_k = d.head_dim <= 64 ? BwdShape<64, true>::LOOP : BwdShape<128, true>::LOOP;
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    snprintf(err, 256, "attention_masked: no CUDA device");
+    return MSLT_ERR_CUDA;
+  }
   TcParams pk = p;
   int rc = map_of(d.q, d, d.heads, AM_ROWS, &mq[0], p.a_perm, err);
-  if (!rc) rc = map_of(d.k, d, d.kv_heads, AB_COLS, &mq[1], p.b_perm, err);
+  if (!rc) rc = map_of(d.k, d, d.kv_heads, BwdShape<64, false>::LOOP, &mq[1], p.b_perm, err);
   if (!rc) rc = map_of(d.dctx, d, d.heads, AM_ROWS, &mq[2], p.c_perm, err);
-  if (!rc) rc = map_of(d.v, d, d.kv_heads, AB_COLS, &mq[3], p.d_perm, err);
+  if (!rc) rc = map_of(d.v, d, d.kv_heads, BwdShape<64, false>::LOOP, &mq[3], p.d_perm, err);
   if (!rc) rc = map_of(d.k, d, d.kv_heads, AM_ROWS, &mk[0], pk.a_perm, err);
-  if (!rc) rc = map_of(d.q, d, d.heads, AB_COLS, &mk[1], pk.b_perm, err);
+  if (!rc) rc = map_of(d.q, d, d.heads, loop_k, &mk[1], pk.b_perm, err);
   if (!rc) rc = map_of(d.v, d, d.kv_heads, AM_ROWS, &mk[2], pk.c_perm, err);
-  if (!rc) rc = map_of(d.dctx, d, d.heads, AB_COLS, &mk[3], pk.d_perm, err);
+  if (!rc) rc = map_of(d.dctx, d, d.heads, loop_k, &mk[3], pk.d_perm, err);
   if (rc) return rc;
   int log_lanes = 0;
   while ((8 << log_lanes) < d.head_dim) log_lanes++;
@@ -1151,10 +1383,12 @@ int attn_masked_tc_bwd(const mslt_attention_desc& d, float* delta, int* status, 
              delta, d.S, d.heads, d.head_dim, log_lanes, rows);
   p.delta = pk.delta = delta;
   p.o0 = view_of(d.dq);
+  p.wide = aligned32(d.dq);
   pk.o0 = view_of(d.dk);
   pk.o1 = view_of(d.dv);
-  rc = backward_of<false>(d, p, mq, st, err);
-  if (!rc) rc = backward_of<true>(d, pk, mk, st, err);
+  pk.wide = aligned32(d.dk) && aligned32(d.dv);
+  rc = backward_of<false>(d, p, mq, sms, st, err);
+  if (!rc) rc = backward_of<true>(d, pk, mk, sms, st, err);
   return rc;
 }
 
