@@ -1142,78 +1142,88 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         if (!mbar_wait(smem_u32(&sfull[j & 1]), j >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
         tc_fence_after();
         const uint32_t tS = trow + (j % SB) * LOOP, tP = trow + Sh::DP_COL + (j % PB) * LOOP;
-        const bool tail = test && it[I_LEN] < first + LOOP;
+        // The step by itself, for blocks without and with pairs to test, 16 columns at a time: 32 need more than the 96
+        // registers that 576 threads have.
+        auto step = [&](auto testing) {
+          constexpr bool kTest = decltype(testing)::value;
+          const bool tail = kTest && it[I_LEN] < first + LOOP;
 #pragma unroll
-        for (int q = 0; q < PART; q += 16) {    // 16 columns at a time: 32 need more than the 96 registers that 576 threads have
-          uint32_t out[kKeys ? 16 : 8];         // keys: P, then dS; queries: dS
-          uint32_t a[16], d[16];
-          tc_ld16_issue(tS + q, a);
-          tc_ld16_issue(tP + q, d);
-          tc_ld16_wait(a);
-          tc_ld16_wait(d);
-          auto read = [&] {
-            if (PB == 1 && q + 16 == PART) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(smem_u32(&dpread));
-            }
-          };
-          if (!test) read();
-          const Piece pc = piece_of<kForm>(f, r, c0 + q, a);
-          const uint32_t seen = see >> q;
-          float most = 0.f;
-          auto gradients = [&](bool tested, auto careful) {
-            choose_way<kForm>(f, pc, tested, [&](auto way) {
-              typedef decltype(way) Wy;
-              float4 nl4, nd4;
-#pragma unroll
-              for (int c = 0; c < 16; c += 2) {
-                float2 x = make_float2(__uint_as_float(a[c]), __uint_as_float(a[c + 1]));
-                float2 t = make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
-                float2 nl = splat2(-lse2), nd = splat2(-delta), bend = splat2(1.f);
-                if (kKeys) {
-                  if (c % 4 == 0) {
-                    nl4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][0][q + c]);
-                    nd4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][1][q + c]);
-                  }
-                  nl = c % 4 ? make_float2(nl4.z, nl4.w) : make_float2(nl4.x, nl4.y);
-                  nd = c % 4 ? make_float2(nd4.z, nd4.w) : make_float2(nd4.x, nd4.y);
-                }
-                x = exponents<Wy, true>(f, pc, x, c, nl, &bend);
-                const bool v0 = !Wy::TEST || (seen >> c & 1), v1 = !Wy::TEST || (seen >> (c + 1) & 1);
-                x.x = ex2(v0 ? x.x : -INFINITY);
-                x.y = ex2(v1 ? x.y : -INFINITY);
-                t = __fmul2_rn(__fadd2_rn(t, nd), x);
-                if (Wy::CAP) t = __fmul2_rn(t, bend);
-                if (Wy::TEST && !decltype(careful)::value) most = fmaxf(most, fmaxf(x.x, x.y));
-                if (decltype(careful)::value) {
-                  t.x = v0 && !(x.x > 0.99999f) ? t.x : 0.f;
-                  t.y = v1 && !(x.y > 0.99999f) ? t.y : 0.f;
-                }
-                if (kKeys) out[c / 2] = pack2(x.x, x.y);
-                out[(kKeys ? 8 : 0) + c / 2] = pack2(t.x, t.y);
-              }
-            });
-          };
-          if (!tail) gradients(test, std::false_type());
-          // Two rare cases are looked at pair by pair.  Columns beyond the sequence, whose dP may be anything.  And a row with a
-          // single key, which has no gradient by its score: dP - delta is the difference of two sums in different orders there,
-          // and is zero in truth.  p(dP_j - delta) is at most (1 - p) times the spread of dP, so nothing above 1e-5 of it
-          // is dropped; a block without pairs to test has as many keys a row as columns, and no such p alone.
-          if (tail || (test && __any_sync(0xffffffffu, most > 0.99999f))) {
-            if (!tail) {  // the first time used them up
+          for (int q = 0; q < PART; q += 16) {
+            uint32_t out[kKeys ? 16 : 8];  // keys: P, then dS; queries: dS
+            uint32_t a[16], d[16];
+            auto load = [&] {
               tc_ld16_issue(tS + q, a);
               tc_ld16_issue(tP + q, d);
               tc_ld16_wait(a);
               tc_ld16_wait(d);
+            };
+            auto read = [&] {
+              if (PB == 1 && q + 16 == PART) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&dpread));
+              }
+            };
+            load();
+            if (!kTest) read();
+            const Piece pc = piece_of<kForm>(f, r, c0 + q, a);
+            const uint32_t seen = see >> q;
+            float most = 0.f;
+            auto gradients = [&](auto careful) {
+              choose_way<kForm>(f, pc, kTest, [&](auto way) {
+                typedef decltype(way) Wy;
+                float4 nl4, nd4;
+#pragma unroll
+                for (int c = 0; c < 16; c += 2) {
+                  float2 x = make_float2(__uint_as_float(a[c]), __uint_as_float(a[c + 1]));
+                  float2 t = make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1]));
+                  float2 nl = splat2(-lse2), nd = splat2(-delta), bend = splat2(1.f);
+                  if (kKeys) {
+                    if (c % 4 == 0) {
+                      nl4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][0][q + c]);
+                      nd4 = *reinterpret_cast<const float4*>(&cols_of[warp - 2][1][q + c]);
+                    }
+                    nl = c % 4 ? make_float2(nl4.z, nl4.w) : make_float2(nl4.x, nl4.y);
+                    nd = c % 4 ? make_float2(nd4.z, nd4.w) : make_float2(nd4.x, nd4.y);
+                  }
+                  x = exponents<Wy, true>(f, pc, x, c, nl, &bend);
+                  const bool v0 = !kTest || (seen >> c & 1), v1 = !kTest || (seen >> (c + 1) & 1);
+                  x.x = ex2(v0 ? x.x : -INFINITY);
+                  x.y = ex2(v1 ? x.y : -INFINITY);
+                  t = __fmul2_rn(__fadd2_rn(t, nd), x);
+                  if (Wy::CAP) t = __fmul2_rn(t, bend);
+                  if (kTest && !decltype(careful)::value) most = fmaxf(most, fmaxf(x.x, x.y));
+                  if (decltype(careful)::value) {
+                    t.x = v0 && !(x.x > 0.99999f) ? t.x : 0.f;
+                    t.y = v1 && !(x.y > 0.99999f) ? t.y : 0.f;
+                  }
+                  if (kKeys) out[c / 2] = pack2(x.x, x.y);
+                  out[(kKeys ? 8 : 0) + c / 2] = pack2(t.x, t.y);
+                }
+              });
+            };
+            if (!kTest) {
+              gradients(std::false_type());
+            } else {
+              // Two rare cases are looked at pair by pair.  Columns beyond the sequence, whose dP may be anything.  And a row with
+              // a single key, which has no gradient by its score: dP - delta is the difference of two sums in different
+              // orders there, and is zero in truth.  p(dP_j - delta) is at most (1 - p) times the spread of dP, so
+              // nothing above 1e-5 of it is dropped; a block without pairs to test has as many keys a row as columns, and
+              // no such p alone.
+              if (!tail) gradients(std::false_type());
+              if (tail || __any_sync(0xffffffffu, most > 0.99999f)) {
+                if (!tail) load();  // the first time used them up
+                gradients(std::true_type());
+              }
+              read();
             }
-            gradients(true, std::true_type());
+            // over the scores that were just read
+            if constexpr (kKeys) tc_st16(tS + q, out);
+            else tc_st8(tS + q, out);
           }
-          if (test) read();
-          // over the scores that were just read
-          if constexpr (kKeys) tc_st16(tS + q, out);
-          else tc_st8(tS + q, out);
-        }
+        };
+        if (test) step(std::true_type());
+        else step(std::false_type());
         tc_st_wait();
         if (test && it[I_LEN] < first + LOOP) {
           // the products' reads of this stage so far are over (S and dP are complete); its rows are an operand once more
