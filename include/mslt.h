@@ -532,15 +532,15 @@ int mslt_op_qk_norm_rope_bwd(const mslt_qk_norm_desc* desc, void* d_scratch, siz
  *     ctx_i = sum_j softmax_j(z_ij) v_j over the keys that query i sees, lse_i = ln sum_j e^(z_ij)
  * A query that sees no key gets ctx 0, lse -infinity and no gradient.  Query head h reads key head h / (heads / kv_heads).
  * Rows at or beyond a sequence's length take no part, whatever they hold (NaN too).
- * bf16: probabilities (relative to the row's maximum) are rounded to bf16 before the product with v, and the row is
- * divided by the sum of what was rounded.  `rest` (bf16, ctx's strides) receives what rounding took off ctx; given to the
+ * bf16: probabilities (relative to a power of two of the row's) are rounded to bf16 before the product with v, and the row
+ * is divided by the sum of what was rounded.  `rest` (bf16, ctx's strides) receives what rounding took off ctx; given to the
  * backward call it makes the rows of the scores' gradient sum to zero also where the keys have much in common.
  * Backward: the gradients of ctx by q, k and v from dctx, ctx, lse (and rest) of the forward call; dk and dv are summed over
  * the query heads that share them, in a fixed order.  The slopes are constants and have no gradient.
  */
 typedef struct {
   void* data;                 /* device; element (b, i, h, e) at data + b * batch + i * row + h * head + e */
-  int64_t batch, row, head;   /* elements; multiples of 16 bytes, as is the address                        */
+  int64_t batch, row, head;   /* elements; multiples of 16 bytes, as is the address (an extent of 1: not used) */
 } mslt_heads;
 typedef struct {
   int32_t dtype;                                  /* 0: fp32, 1: bf16                          */

@@ -9,6 +9,22 @@ using namespace mslt;
 
 namespace {
 
+// The strides of a single sequence, row or head are not used; they become ones that suit a tensor map.
+mslt_heads tidy(const mslt_heads& h, const mslt_attention_desc& d, int heads) {
+  mslt_heads t = h;
+  if (d.B == 1) t.batch = 0;
+  if (d.S == 1) t.row = 128;
+  if (heads == 1) t.head = 0;
+  return t;
+}
+mslt_attention_desc tidy(const mslt_attention_desc& d) {
+  mslt_attention_desc t = d;
+  t.q = tidy(d.q, d, d.heads); t.ctx = tidy(d.ctx, d, d.heads); t.dctx = tidy(d.dctx, d, d.heads); t.dq = tidy(d.dq, d, d.heads);
+  t.k = tidy(d.k, d, d.kv_heads); t.v = tidy(d.v, d, d.kv_heads); t.dk = tidy(d.dk, d, d.kv_heads); t.dv = tidy(d.dv, d, d.kv_heads);
+  return t;
+}
+
+// h: tidied
 int check_heads(const char* what, const char* name, const mslt_heads& h, int dtype) {
   const int unit = dtype == 1 ? 8 : 4;
   if (!h.data) return op_refuse(MSLT_ERR_ARG, "%s: %s is null", what, name);
@@ -19,7 +35,7 @@ int check_heads(const char* what, const char* name, const mslt_heads& h, int dty
 }
 
 int check_attention(const char* what, const mslt_attention_desc* d, const int32_t* status) {
-  if (!d || !status) return op_refuse(MSLT_ERR_ARG, "%s: null pointer", what);
+  if (!status) return op_refuse(MSLT_ERR_ARG, "%s: null pointer", what);
   if (d->dtype != 0 && d->dtype != 1) return op_refuse(MSLT_ERR_ARG, "%s: dtype must be 0 or 1", what);
   if (d->B < 1 || d->S < 1 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads)
     return op_refuse(MSLT_ERR_ARG, "%s: needs B, S, heads >= 1 and heads a multiple of kv_heads", what);
@@ -53,8 +69,10 @@ int end_attention(const char* what, const int32_t* status, cudaStream_t st, int 
 
 extern "C" {
 
-int mslt_op_attention_masked(const mslt_attention_desc* desc, int32_t* d_status, void* cuda_stream, int32_t sync) {
+int mslt_op_attention_masked(const mslt_attention_desc* caller, int32_t* d_status, void* cuda_stream, int32_t sync) {
   const char* what = "attention_masked";
+  if (!caller) return op_refuse(MSLT_ERR_ARG, "%s: null pointer", what);
+  const mslt_attention_desc given = tidy(*caller), *desc = &given;
   int rc = check_attention(what, desc, d_status);
   if (rc || (rc = op_need_device())) return rc;
   return op_nothrow(what, [&] {
@@ -71,9 +89,11 @@ size_t mslt_op_attention_masked_bwd_scratch_bytes(int32_t B, int32_t S, int32_t 
   return ((size_t)B * S * heads * sizeof(float) + 255) / 256 * 256;
 }
 
-int mslt_op_attention_masked_bwd(const mslt_attention_desc* desc, void* d_scratch, size_t scratch_bytes, int32_t* d_status,
+int mslt_op_attention_masked_bwd(const mslt_attention_desc* caller, void* d_scratch, size_t scratch_bytes, int32_t* d_status,
                                  void* cuda_stream, int32_t sync) {
   const char* what = "attention_masked_bwd";
+  if (!caller) return op_refuse(MSLT_ERR_ARG, "%s: null pointer", what);
+  const mslt_attention_desc given = tidy(*caller), *desc = &given;
   int rc = check_attention(what, desc, d_status);
   if (rc) return rc;
   if ((rc = check_heads(what, "dctx", desc->dctx, desc->dtype)) || (rc = check_heads(what, "dq", desc->dq, desc->dtype)) ||

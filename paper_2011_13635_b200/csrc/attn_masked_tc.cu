@@ -42,12 +42,12 @@ constexpr int AB_SOFT = 16, AB_THREADS = 64 + 32 * AB_SOFT;  // backward
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // A row's exponents are relative to a reference: the largest score of the first block in which it sees anything, without its
 // bias, rounded up to a whole number (capped scores: none).  Later blocks take no maximum: range is what counts and not
-// size, and a row whose probabilities do not add up to something between 2^-64 and 2^90 is the rare exception.  A block with
+// size, and a row whose probabilities do not add up to something between 2^-64 and 2^64 is the rare exception.  A block with
 // such a row goes over its loop again, this time with a running maximum; the reference then moves by whole powers of two,
 // so what is there so far is scaled without rounding.  (With a running maximum throughout, a loop block of four
 // blocks an SM spent 550 of 2900 cycles on it, and its scores were read a third time; sums tested against the limit block
 // by block still cost 450 cycles of a block alone on its SM, 85 of 940 of the SM.)
-constexpr float AM_MOST = 1.2379400392853803e27f, AM_LEAST = 5.421010862427522e-20f;  // 2^90, 2^-64
+constexpr float AM_MOST = 1.8446744073709552e19f, AM_LEAST = 5.421010862427522e-20f;  // 2^64, 2^-64
 
 struct View { bf16* p; long long batch, row, head; };
 struct TcParams {
@@ -558,8 +558,8 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   const Form f = form_of<kForm>(p.m, h);
   const int* docs = p.m.docs ? p.m.docs + (long long)b * p.m.S : nullptr;
   const int doc = docs && r < s.len ? docs[r] : 0;
-  // Capped scores lie in [-cap, cap]: a cap of up to 44 (2^64) needs no reference.
-  const bool fixed = kForm == 2 && f.cap2 <= 64.f && f.slope2 >= 0.f;
+  // Capped scores lie in [-cap, cap]: a cap of up to 30 (2^44, and 2^17 keys) needs no reference.
+  const bool fixed = kForm == 2 && f.cap2 <= 44.f && f.slope2 >= 0.f;
   float top = 0.f;                                                      // reference of the row's exponents, a whole number
   float2 sum = make_float2(0.f, 0.f), exact = make_float2(0.f, 0.f);   // of the rounded probabilities, and of the unrounded ones
   bool ok = true;

@@ -120,16 +120,18 @@ __device__ __forceinline__ void rotate(float (&a)[W], float (&b)[W], const float
 // backward queries and keys are taken by different blocks (grid y), each with one set of sums in registers.
 // PASSES, and BLOCKS of 256 threads on an SM (80 or 128 registers), were tried together; 16384 rows x 24 heads x 64 and 8144 x 20
 // x 128, us: rotation 3 x 4 18.8 and 16.2, 3 x 3 19.7 and 18.5, 2 x 3 21.6 and 18.5; norm 2 x 3 25.6 and 23.9, 3 x 3 32 and
-// 27, 3 x 2 27 and 28; backward 3 x 2 44 and 43, 2 x 3 54 and 40.  Asking for a row ahead gained nothing at any of them.
-template <int OP> struct Shape {
-  static constexpr int PASSES = OP == 1 ? 2 : 3, BLOCKS = OP == 0 ? 4 : OP == 1 ? 3 : 2;
+// 27, 3 x 2 27 and 28; backward 3 x 2 44 and 43, 2 x 3 54 and 40.  Rotation in fp32, 8168 x 32 x 64:
+// 4 x 2 24.5, 2 x 3 24.9, 4 x 3 28.4, 3 x 4 31.1.  Asking for a row ahead gained nothing at any of them.
+template <typename T, int OP> struct Shape {
+  static constexpr bool wide = sizeof(T) == 4 && OP == 0;
+  static constexpr int PASSES = wide ? 4 : OP == 1 ? 2 : 3, BLOCKS = wide ? 2 : OP == 0 ? 4 : OP == 1 ? 3 : 2;
 };
 
 template <typename T, bool INTER, int OP>
-__global__ void __launch_bounds__(32 * RO_WARPS, Shape<OP>::BLOCKS)
+__global__ void __launch_bounds__(32 * RO_WARPS, (Shape<T, OP>::BLOCKS))
 rotary_kernel(const RotaryParams p) {
   constexpr bool kExact = sizeof(T) == 4;
-  constexpr int PASSES = Shape<OP>::PASSES;
+  constexpr int PASSES = Shape<T, OP>::PASSES;
   typedef Piece<T> Pc;
   typedef typename Pc::Raw Raw;
   __shared__ __align__(16) uint64_t turns[64];
@@ -377,7 +379,8 @@ RotaryLaunch plan_rotary(RotaryParams& p, int most_passes, int blocks_per_sm, in
 
 template <int OP>
 RotaryLaunch run_rotary(const mslt_rope_desc& d, RotaryParams& p, int sms, cudaStream_t st) {
-  const RotaryLaunch l = plan_rotary(p, Shape<OP>::PASSES, Shape<OP>::BLOCKS, sms, OP == 2);
+  const RotaryLaunch l = d.dtype == 1 ? plan_rotary(p, Shape<bf16, OP>::PASSES, Shape<bf16, OP>::BLOCKS, sms, OP == 2)
+                                      : plan_rotary(p, Shape<float, OP>::PASSES, Shape<float, OP>::BLOCKS, sms, OP == 2);
   if (d.dtype == 1) {
     if (d.interleaved) launch_pdl(rotary_kernel<bf16, true, OP>, l.grid, 32 * RO_WARPS, 0, st, p);
     else launch_pdl(rotary_kernel<bf16, false, OP>, l.grid, 32 * RO_WARPS, 0, st, p);
@@ -388,7 +391,11 @@ RotaryLaunch run_rotary(const mslt_rope_desc& d, RotaryParams& p, int sms, cudaS
   return l;
 }
 
-int check_strided(const char* what, const char* name, int dtype, const void* ptr, int64_t row, int64_t head) {
+// the strides of a single row and of a single head are not used
+int check_strided(const char* what, const char* name, const mslt_rope_desc& d, const void* ptr, int64_t row, int64_t head) {
+  const int dtype = d.dtype;
+  if (d.rows == 1) row = 0;
+  if (d.heads == 1) head = 0;
   const int unit = dtype == 1 ? 8 : 4;
   if (!ptr) return op_refuse(MSLT_ERR_ARG, "%s: %s is null", what, name);
   if ((uintptr_t)ptr & 15) return op_refuse(MSLT_ERR_ARG, "%s: %s must be 16-byte aligned", what, name);
@@ -401,7 +408,7 @@ int check_rope(const char* what, const mslt_rope_desc* d, int rot_min) {
   if (!d) return op_refuse(MSLT_ERR_ARG, "%s: null descriptor", what);
   if (d->dtype != 0 && d->dtype != 1) return op_refuse(MSLT_ERR_ARG, "%s: dtype must be 0 or 1", what);
   if (d->rows < 1 || d->heads < 1) return op_refuse(MSLT_ERR_ARG, "%s: rows and heads must be >= 1", what);
-  if (d->heads > 4096) return op_refuse(MSLT_ERR_SIZE, "%s: at most 4096 heads", what);
+  if (d->heads > 4096 || d->rows > (1 << 30)) return op_refuse(MSLT_ERR_SIZE, "%s: at most 4096 heads and 2^30 rows", what);
   if (d->head_dim < 8 || d->head_dim > 128 || d->head_dim % 8)
     return op_refuse(MSLT_ERR_ARG, "%s: head_dim must be a multiple of 8 in [8, 128]", what);
   if (d->rot_dim < rot_min || d->rot_dim > d->head_dim || d->rot_dim % 8)
@@ -410,7 +417,7 @@ int check_rope(const char* what, const mslt_rope_desc* d, int rot_min) {
     return op_refuse(MSLT_ERR_ARG, "%s: turns must be 16-byte aligned and not null", what);
   if (!d->positions && d->seq < 1) return op_refuse(MSLT_ERR_ARG, "%s: without positions seq must be >= 1", what);
   if (!isfinite(d->magnitude)) return op_refuse(MSLT_ERR_ARG, "%s: magnitude must be finite", what);
-  return check_strided(what, "x", d->dtype, d->x, d->x_row, d->x_head);
+  return check_strided(what, "x", *d, d->x, d->x_row, d->x_head);
 }
 
 void fill_rope(const mslt_rope_desc& d, RotaryParams& p) {
@@ -480,7 +487,7 @@ int mslt_rope_turns(int32_t rot_dim, double base, int32_t scaling, double factor
 int mslt_op_rope(const mslt_rope_desc* desc, void* cuda_stream, int32_t sync) {
   int rc = check_rope("rope", desc, 8);
   if (rc) return rc;
-  rc = check_strided("rope", "y", desc->dtype, desc->y, desc->y_row, desc->y_head);
+  rc = check_strided("rope", "y", *desc, desc->y, desc->y_row, desc->y_head);
   if (rc) return rc;
   int sms = 0;
   if ((rc = op_need_device()) || (rc = sm_count(&sms))) return rc;
@@ -493,7 +500,7 @@ int mslt_op_rope(const mslt_rope_desc* desc, void* cuda_stream, int32_t sync) {
 int mslt_op_qk_norm_rope(const mslt_qk_norm_desc* desc, void* cuda_stream, int32_t sync) {
   int rc = check_norm("qk_norm_rope", desc);
   if (rc) return rc;
-  rc = check_strided("qk_norm_rope", "y", desc->rope.dtype, desc->rope.y, desc->rope.y_row, desc->rope.y_head);
+  rc = check_strided("qk_norm_rope", "y", desc->rope, desc->rope.y, desc->rope.y_row, desc->rope.y_head);
   if (rc) return rc;
   int sms = 0;
   if ((rc = op_need_device()) || (rc = sm_count(&sms))) return rc;
@@ -515,8 +522,8 @@ int mslt_op_qk_norm_rope_bwd(const mslt_qk_norm_desc* desc, void* d_scratch, siz
   const char* what = "qk_norm_rope_bwd";
   int rc = check_norm(what, desc);
   if (rc) return rc;
-  if ((rc = check_strided(what, "dy", desc->rope.dtype, desc->dy, desc->dy_row, desc->dy_head))) return rc;
-  if ((rc = check_strided(what, "dx", desc->rope.dtype, desc->dx, desc->dx_row, desc->dx_head))) return rc;
+  if ((rc = check_strided(what, "dy", desc->rope, desc->dy, desc->dy_row, desc->dy_head))) return rc;
+  if ((rc = check_strided(what, "dx", desc->rope, desc->dx, desc->dx_row, desc->dx_head))) return rc;
   if (!desc->dgain) return op_refuse(MSLT_ERR_ARG, "%s: dgain is null", what);
   const size_t need = mslt_op_qk_norm_rope_bwd_scratch_bytes(desc->rope.rows, desc->rope.heads, desc->rope.head_dim);
   if (!d_scratch || scratch_bytes < need || ((uintptr_t)d_scratch & 15))

@@ -196,6 +196,88 @@ def test_against_the_formula(dtype, kw):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("how", ["rising", "falling", "steep", "uphill", "far", "negative", "zero", "capped", "capped_biased"])
+def test_scores_of_every_range(dtype, dim, how):
+    """Rows whose first block says nothing of what is to come: scores that rise or fall by hundreds along the keys, steep
+    biases either way, keys that are all far away, scales that are not positive, caps beyond every score's range."""
+    import torch
+    n = 333
+    kw = dict(rising={}, falling={}, steep=dict(slopes=True), uphill=dict(slopes=True, causal=True), far=dict(slopes=True, docs=(np.arange(n) % 300)[None]),
+              negative=dict(causal=True), zero={}, capped=dict(cap=80.0), capped_biased=dict(cap=25.0, slopes=True, causal=True))[how]
+    s = make(dtype, 1, n, 2, 1, dim, seed=9, **kw)
+    if how in ("rising", "falling", "capped"):
+        along = torch.linspace(0, 30, n, device="cuda")[None, :, None, None] * (-1 if how == "falling" else 1)
+        s["q"] = (s["q"].float().abs() + 0.5).to(s["q"].dtype)
+        s["k"] = (s["k"].float() * 0.3 + along / dim ** 0.5).to(s["k"].dtype)       # a row's scores run over some 150
+    if how == "steep":
+        s["mask"]["slopes"] = torch.tensor([30.0, 2.5], device="cuda")
+    if how == "uphill":
+        s["mask"]["slopes"] = torch.tensor([-1.0, -0.01], device="cuda")
+    if how == "far":        # every document's tokens are 300 apart: all biases but the own token's are below -600
+        s["mask"]["slopes"] = torch.tensor([2.0, 0.6], device="cuda")
+    if how in ("negative", "zero"):
+        s["scale"] = -0.2 if how == "negative" else 0.0
+    # |scale| in the bounds
+    sign = math.copysign(1.0, s["scale"])
+    if sign < 0:
+        ref = dict(s, q=-s["q"], scale=-s["scale"])
+        out = run(s)
+        check(ref, dict(out, dq=-out["dq"]))
+    else:
+        check(s, run(s))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_single_key_has_no_gradient_by_its_score(dtype, dim):
+    import torch
+    for kw in (dict(S=1), dict(S=150, docs=np.arange(150)[None].repeat(3, 0)), dict(S=70, lens=[1, 1, 1])):
+        s = make(dtype, 3, heads=4, kv=2, dim=dim, slopes=True, **kw)
+        out = run(s)
+        assert not out["dq"].any() and not out["dk"].any()
+        check(s, out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_layouts(dtype):
+    """Heads before rows, padded rows on 16-byte boundaries only, and strides of single extents that nobody reads."""
+    import torch
+    s = make(dtype, 2, 140, 4, 2, 64, docs=documents(2, 140, 2))
+    want = run(s)
+    pad = 8 if dtype == "bf16" else 4
+
+    def moved(x):      # [B, heads, S, dim + pad] storage, offset by 16 bytes
+        b, n, h, d = x.shape
+        store = torch.empty(b * h * n * (d + pad) + pad, dtype=x.dtype, device="cuda")[pad:]
+        y = store.view(b, h, n, d + pad)[..., :d].transpose(1, 2)
+        y.copy_(x)
+        return y
+    t = dict(s, **{k: moved(s[k]) for k in ("q", "k", "v", "dc")})
+    got = run(t)
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    one = make(dtype, 1, 1, 1, 1, 64)
+    odd = dict(one, **{k: one[k].as_strided((1, 1, 1, 64), (3, 5, 7, 1)) for k in ("q", "k", "v", "dc")})
+    a, b = run(one), run(odd)
+    for k in a:
+        assert torch.equal(a[k], b[k]), k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_short_and_empty_sequences(dtype, dim):
+    """More row tiles than the device has SMs, most of them without a step."""
+    lens = [(17 * i) % 150 if i % 3 == 0 else 0 for i in range(90)]
+    s = make(dtype, 90, 140, 2, 1, dim, lens=lens, causal=True)
+    check(s, run(s))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_evaluation_alone(dtype):
     """Without lse and rest, as an evaluation calls it: the same context."""
     import torch

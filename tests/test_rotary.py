@@ -106,7 +106,7 @@ def test_refusals_before_any_device():
            dict(turns=8), dict(seq=0), dict(magnitude=float("inf"))]
     for change in bad:
         assert rc(B.lib.mslt_op_rope, **change) == -1, change
-    assert rc(B.lib.mslt_op_rope, heads=5000) == -2
+    assert rc(B.lib.mslt_op_rope, heads=5000) == -2 and rc(B.lib.mslt_op_rope, rows=(1 << 30) + 1) == -2
     assert B.lib.mslt_op_rope(None, None, 1) == -1
     size = B.mslt_op_qk_norm_rope_bwd_scratch_bytes(4, 2, 64)
     fwd = lambda n: B.lib.mslt_op_qk_norm_rope(B.C.byref(n), None, 1)                                       # noqa: E731
