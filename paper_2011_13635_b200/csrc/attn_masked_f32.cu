@@ -6,7 +6,7 @@
 //             dK = scale dS^T Q and dV = P^T dC by blocks of keys, over all query heads that share them
 // A block owns 32 rows, 128 threads hold 4 x 4 scores each, then 4 rows x 4 (8) columns of the accumulators, as packed
 // multiply-adds.  32 rows and not 64 because full precision is used on small batches, whose blocks have to fill the device:
-// 2 x 12 heads x 509 keys in 3 documents, forward | backward, 81 | 264 us with 64 rows and plain loads, 69 | 173 us so.  The
+// 2 x 12 heads x 509 keys in 3 documents, forward | backward, 81 | 264 us with 64 rows and plain loads, 65 | 165 us so.  The
 // other side's tiles of 64 rows are asked for by asynchronous copies as soon as the product before is done with their memory.
 // A tile is left out where the mask leaves none of its pairs (attn_masked.h).  Rows beyond a sequence are zero in shared memory.
 // delta is summed in the order in which dP is, so that where a query sees a single key dP - delta is exactly zero.
@@ -22,7 +22,8 @@ namespace {
 
 constexpr int MF_R = 32;         // rows of a block
 constexpr int MF_C = 64;         // rows of a tile of the other side
-constexpr int MF_NT = 128;
+constexpr int MF_RPT = 4;        // rows of a thread (2 on twice the threads: backward 165 -> 227 us, the reads of operands decide)
+constexpr int MF_NT = 16 * MF_R / MF_RPT;
 constexpr int MF_PP = MF_C + 4;  // floats between rows of a tile of scores
 
 struct Rows { const float* p; int64_t batch, row, head; };
@@ -59,23 +60,23 @@ __device__ __forceinline__ void landed() {
   __syncthreads();
 }
 
-// s[i][c] = row 4 ty + i of A . row tx + 16 c of B, even and odd elements summed apart
+// s[i][c] = row MF_RPT ty + i of A . row tx + 16 c of B, even and odd elements summed apart
 template <int DP>
-__device__ __forceinline__ void products(const float* A, const float* B, int ty, int tx, float (&s)[4][4]) {
-  float2 acc[4][4];
+__device__ __forceinline__ void products(const float* A, const float* B, int ty, int tx, float (&s)[MF_RPT][4]) {
+  float2 acc[MF_RPT][4];
 #pragma unroll
-  for (int i = 0; i < 4; i++)
+  for (int i = 0; i < MF_RPT; i++)
 #pragma unroll
     for (int c = 0; c < 4; c++) acc[i][c] = make_float2(0.f, 0.f);
 #pragma unroll 4
   for (int e = 0; e < DP; e += 4) {
-    float4 a[4], b[4];
+    float4 a[MF_RPT], b[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) a[i] = *reinterpret_cast<const float4*>(A + (4 * ty + i) * (DP + 4) + e);
+    for (int i = 0; i < MF_RPT; i++) a[i] = *reinterpret_cast<const float4*>(A + (MF_RPT * ty + i) * (DP + 4) + e);
 #pragma unroll
     for (int c = 0; c < 4; c++) b[c] = *reinterpret_cast<const float4*>(B + (tx + 16 * c) * (DP + 4) + e);
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int i = 0; i < MF_RPT; i++)
 #pragma unroll
       for (int c = 0; c < 4; c++) {
         acc[i][c] = __ffma2_rn(make_float2(a[i].x, a[i].y), make_float2(b[c].x, b[c].y), acc[i][c]);
@@ -83,26 +84,26 @@ __device__ __forceinline__ void products(const float* A, const float* B, int ty,
       }
   }
 #pragma unroll
-  for (int i = 0; i < 4; i++)
+  for (int i = 0; i < MF_RPT; i++)
 #pragma unroll
     for (int c = 0; c < 4; c++) s[i][c] = acc[i][c].x + acc[i][c].y;
 }
 
-// acc row 4 ty + i, columns 4 tx + 64 j.. += sum over the rows of B of P[row][n] B[n][column]
+// acc row MF_RPT ty + i, columns 4 tx + 64 j.. += sum over the rows of B of P[row][n] B[n][column]
 template <int DP>
-__device__ __forceinline__ void accumulate(const float* P, const float* B, int ty, int tx, float2 (&acc)[4][DP / 64][2]) {
+__device__ __forceinline__ void accumulate(const float* P, const float* B, int ty, int tx, float2 (&acc)[MF_RPT][DP / 64][2]) {
 #pragma unroll 4
   for (int n = 0; n < MF_C; n += 4) {
-    float4 p[4];
+    float4 p[MF_RPT];
 #pragma unroll
-    for (int i = 0; i < 4; i++) p[i] = *reinterpret_cast<const float4*>(P + (4 * ty + i) * MF_PP + n);
+    for (int i = 0; i < MF_RPT; i++) p[i] = *reinterpret_cast<const float4*>(P + (MF_RPT * ty + i) * MF_PP + n);
 #pragma unroll
     for (int k = 0; k < 4; k++)
 #pragma unroll
       for (int j = 0; j < DP / 64; j++) {
         const float4 b = *reinterpret_cast<const float4*>(B + (n + k) * (DP + 4) + 64 * j + 4 * tx);
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
+        for (int i = 0; i < MF_RPT; i++) {
           const float w = k == 0 ? p[i].x : k == 1 ? p[i].y : k == 2 ? p[i].z : p[i].w;
           acc[i][j][0] = __ffma2_rn(make_float2(w, w), make_float2(b.x, b.y), acc[i][j][0]);
           acc[i][j][1] = __ffma2_rn(make_float2(w, w), make_float2(b.z, b.w), acc[i][j][1]);
@@ -125,16 +126,45 @@ __device__ __forceinline__ float half_sum(float v) {
 __device__ __forceinline__ bool sees(const Seq& s, int i, int j, int di, int dj) {
   return i < s.len && j < s.len && di == dj && (j <= i || j < s.prefix);
 }
-// the score behind cap and bias; bend: the cap's derivative
-__device__ __forceinline__ float score(const AttnMask& m, float slope, float dot, int i, int j, float* bend) {
-  float z = dot * m.scale;
-  *bend = 1.f;
+// The scores behind cap, bias and mask (where test: others -infinity); bend: the cap's derivative.  Rows i0 + i, columns
+// j0 + 16 c.  Exponentials further down are 2^x of the hardware (relative error 2^-22) of a rounded x log2(e): what that
+// costs grows with |x|, as the probability falls.
+template <bool kKeys>
+__device__ __forceinline__ void scores(const AttnMask& m, const Seq& s, float slope, bool test, int i0, int j0, const int* idocs,
+                                       const int* jdocs, float (&z)[MF_RPT][4], float (&bend)[MF_RPT][4]) {
+#pragma unroll
+  for (int i = 0; i < MF_RPT; i++)
+#pragma unroll
+    for (int c = 0; c < 4; c++) {
+      z[i][c] *= m.scale;
+      bend[i][c] = 1.f;
+    }
   if (m.cap > 0.f) {
-    const float t = tanhf(z / m.cap);
-    z = m.cap * t;
-    *bend = 1.f - t * t;
+#pragma unroll
+    for (int i = 0; i < MF_RPT; i++)
+#pragma unroll
+      for (int c = 0; c < 4; c++) {
+        const float t = tanhf(z[i][c] / m.cap);
+        z[i][c] = m.cap * t;
+        bend[i][c] = 1.f - t * t;
+      }
   }
-  return z - slope * fabsf((float)(i - j));
+  if (m.slopes) {
+#pragma unroll
+    for (int i = 0; i < MF_RPT; i++)
+#pragma unroll
+      for (int c = 0; c < 4; c++) z[i][c] -= slope * fabsf((float)(i0 + i - j0 - 16 * c));
+  }
+  if (test) {
+#pragma unroll
+    for (int i = 0; i < MF_RPT; i++)
+#pragma unroll
+      for (int c = 0; c < 4; c++) {
+        const int a = i0 + i, b = j0 + 16 * c;
+        const bool ok = kKeys ? sees(s, b, a, jdocs[16 * c], idocs[i]) : sees(s, a, b, idocs[i], jdocs[16 * c]);
+        z[i][c] = ok ? z[i][c] : -INFINITY;
+      }
+  }
 }
 
 __device__ __forceinline__ int document(const AttnMask& m, const Seq& s, int b, int r) {
@@ -143,10 +173,10 @@ __device__ __forceinline__ int document(const AttnMask& m, const Seq& s, int b, 
 
 template <int DP>
 __device__ __forceinline__ void store_rows(const Rows& dst, int b, int r0, int h, int S, int D, int ty, int tx,
-                                           const float2 (&acc)[4][DP / 64][2], const float (&f)[4]) {
+                                           const float2 (&acc)[MF_RPT][DP / 64][2], const float (&f)[MF_RPT]) {
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const int r = r0 + 4 * ty + i;
+  for (int i = 0; i < MF_RPT; i++) {
+    const int r = r0 + MF_RPT * ty + i;
     if (r >= S) continue;
     float* out = const_cast<float*>(row_ptr(dst, b, r, h));
 #pragma unroll
@@ -184,10 +214,10 @@ masked_fwd_kernel(const MaskedParams p) {
   ask_tile<DP, MF_R>(Qs, p.q, b, q0, h, s.len, p.D);
   if (threadIdx.x < MF_R) qdocs[threadIdx.x] = document(p.m, s, b, q0 + threadIdx.x);
   const int n = list_blocks<false, MF_NT / 32, MF_R, MF_C>(p.m, s, b, q0, list, red);
-  float2 acc[4][DP / 64][2];
-  float top[4], sum[4];
+  float2 acc[MF_RPT][DP / 64][2];
+  float top[MF_RPT], sum[MF_RPT];
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
+  for (int i = 0; i < MF_RPT; i++) {
     top[i] = -INFINITY;
     sum[i] = 0.f;
 #pragma unroll
@@ -209,31 +239,28 @@ masked_fwd_kernel(const MaskedParams p) {
     const bool test = list[j] & 1;
     if (threadIdx.x < MF_C) kdocs[threadIdx.x] = doc;
     landed<1>();
-    float z[4][4];
+    float z[MF_RPT][4];
     products<DP>(Qs, Ks, ty, tx, z);
     __syncthreads();
     if (j + 1 < n) ask_k(j + 1);
     else asm volatile("cp.async.commit_group;" ::: "memory");
+    float bend[MF_RPT][4];
+    scores<false>(p.m, s, slope, test, q0 + MF_RPT * ty, k0 + tx, qdocs + MF_RPT * ty, kdocs + tx, z, bend);
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
+    for (int i = 0; i < MF_RPT; i++) {
       float t = top[i];
 #pragma unroll
-      for (int c = 0; c < 4; c++) {
-        const int qi = q0 + 4 * ty + i, kj = k0 + tx + 16 * c;
-        float bend;
-        z[i][c] = !test || sees(s, qi, kj, qdocs[4 * ty + i], kdocs[tx + 16 * c]) ? score(p.m, slope, z[i][c], qi, kj, &bend) : -INFINITY;
-        t = fmaxf(t, z[i][c]);
-      }
+      for (int c = 0; c < 4; c++) t = fmaxf(t, z[i][c]);
       t = half_max(t);
       const float base = t == -INFINITY ? 0.f : t;
-      const float keep = expf(top[i] - base);
+      const float keep = __expf(top[i] - base);
       top[i] = t;
       float part = 0.f;
 #pragma unroll
       for (int c = 0; c < 4; c++) {
-        const float e = expf(z[i][c] - base);
+        const float e = __expf(z[i][c] - base);
         part += e;
-        Ps[(4 * ty + i) * MF_PP + tx + 16 * c] = e;
+        Ps[(MF_RPT * ty + i) * MF_PP + tx + 16 * c] = e;
       }
       sum[i] = sum[i] * keep + half_sum(part);
 #pragma unroll
@@ -247,11 +274,11 @@ masked_fwd_kernel(const MaskedParams p) {
     __syncthreads();
     if (j + 1 < n) ask_v(j + 1);
   }
-  float f[4];
+  float f[MF_RPT];
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
+  for (int i = 0; i < MF_RPT; i++) {
     f[i] = sum[i] > 0.f ? 1.f / sum[i] : 0.f;
-    const int r = q0 + 4 * ty + i;
+    const int r = q0 + MF_RPT * ty + i;
     const bool dead = r >= s.len;  // its row of Q is zero and may have been given scores where nothing is tested
     if (dead) f[i] = 0.f;
     if (tx == 0 && p.lse && r < p.m.S) p.lse[((int64_t)b * p.heads + h) * p.m.S + r] = dead ? -INFINITY : top[i] + logf(sum[i]);
@@ -300,11 +327,11 @@ masked_dq_kernel(const MaskedParams p) {
   ask_tile<DP, MF_R>(Cs, p.dc, b, q0, h, s.len, p.D);
   if (threadIdx.x < MF_R) qdocs[threadIdx.x] = document(p.m, s, b, q0 + threadIdx.x);
   const int n = list_blocks<false, MF_NT / 32, MF_R, MF_C>(p.m, s, b, q0, list, red);
-  float2 acc[4][DP / 64][2];
-  float lse[4], delta[4];
+  float2 acc[MF_RPT][DP / 64][2];
+  float lse[MF_RPT], delta[MF_RPT];
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const int r = q0 + 4 * ty + i;
+  for (int i = 0; i < MF_RPT; i++) {
+    const int r = q0 + MF_RPT * ty + i;
     const int64_t at = ((int64_t)b * p.heads + h) * p.m.S + r;
     lse[i] = r < s.len ? p.lse[at] : INFINITY;  // no probability
     delta[i] = r < s.len ? p.delta[at] : 0.f;
@@ -326,31 +353,29 @@ masked_dq_kernel(const MaskedParams p) {
     const int k0 = (list[j] >> 1) * MF_C;
     const bool test = list[j] & 1;
     if (threadIdx.x < MF_C) kdocs[threadIdx.x] = doc;
-    float z[4][4], dp[4][4];
+    float z[MF_RPT][4], dp[MF_RPT][4];
     landed<1>();
     products<DP>(Cs, Vs, ty, tx, dp);
     landed<0>();
     if (j + 1 < n) ask_v(j + 1);
     products<DP>(Qs, Ks, ty, tx, z);
+    float bend[MF_RPT][4];
+    scores<false>(p.m, s, slope, test, q0 + MF_RPT * ty, k0 + tx, qdocs + MF_RPT * ty, kdocs + tx, z, bend);
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int i = 0; i < MF_RPT; i++)
 #pragma unroll
       for (int c = 0; c < 4; c++) {
-        const int qi = q0 + 4 * ty + i, kj = k0 + tx + 16 * c;
-        float ds = 0.f;
-        if (!test || sees(s, qi, kj, qdocs[4 * ty + i], kdocs[tx + 16 * c])) {
-          float bend;
-          const float w = expf(score(p.m, slope, z[i][c], qi, kj, &bend) - lse[i]);
-          ds = w * (dp[i][c] - delta[i]) * bend;
-        }
-        Ps[(4 * ty + i) * MF_PP + tx + 16 * c] = ds;
+        const float w = __expf(z[i][c] - lse[i]);
+        Ps[(MF_RPT * ty + i) * MF_PP + tx + 16 * c] = w > 0.f ? w * (dp[i][c] - delta[i]) * bend[i][c] : 0.f;
       }
     __syncwarp();  // the scores of a thread's rows are its half warp's
     accumulate<DP>(Ps, Ks, ty, tx, acc);
     __syncthreads();
     if (j + 1 < n) ask_k(j + 1);
   }
-  const float f[4] = {p.m.scale, p.m.scale, p.m.scale, p.m.scale};
+  float f[MF_RPT];
+#pragma unroll
+  for (int i = 0; i < MF_RPT; i++) f[i] = p.m.scale;
   store_rows<DP>(p.o0, b, q0, h, p.m.S, p.D, ty, tx, acc, f);
 }
 
@@ -377,9 +402,9 @@ masked_dkv_kernel(const MaskedParams p) {
   ask_tile<DP, MF_R>(Vs, p.v, b, k0, hk, s.len, p.D);
   if (threadIdx.x < MF_R) kdocs[threadIdx.x] = document(p.m, s, b, k0 + threadIdx.x);
   const int n = list_blocks<true, MF_NT / 32, MF_R, MF_C>(p.m, s, b, k0, list, red);
-  float2 dk[4][DP / 64][2], dv[4][DP / 64][2];
+  float2 dk[MF_RPT][DP / 64][2], dv[MF_RPT][DP / 64][2];
 #pragma unroll
-  for (int i = 0; i < 4; i++)
+  for (int i = 0; i < MF_RPT; i++)
 #pragma unroll
     for (int j = 0; j < DP / 64; j++) dk[i][j][0] = dk[i][j][1] = dv[i][j][0] = dv[i][j][1] = make_float2(0.f, 0.f);
   // steps: the list once for every query head that shares the keys
@@ -410,24 +435,21 @@ masked_dkv_kernel(const MaskedParams p) {
       lses[threadIdx.x] = lse;
       deltas[threadIdx.x] = delta;
     }
-    float z[4][4], dp[4][4];
+    float z[MF_RPT][4], dp[MF_RPT][4];
     landed<1>();
     products<DP>(Vs, Cs, ty, tx, dp);
     landed<0>();
     products<DP>(Ks, Qs, ty, tx, z);
+    float bend[MF_RPT][4];
+    scores<true>(p.m, s, slope, test, k0 + MF_RPT * ty, q0 + tx, kdocs + MF_RPT * ty, qdocs + tx, z, bend);
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int i = 0; i < MF_RPT; i++)
 #pragma unroll
       for (int c = 0; c < 4; c++) {
-        const int m = tx + 16 * c, qi = q0 + m, kj = k0 + 4 * ty + i;
-        float w = 0.f, ds = 0.f;
-        if (!test || sees(s, qi, kj, qdocs[m], kdocs[4 * ty + i])) {
-          float bend;
-          w = expf(score(p.m, slope, z[i][c], qi, kj, &bend) - lses[m]);
-          ds = w * (dp[i][c] - deltas[m]) * bend;
-        }
-        Ps[(4 * ty + i) * MF_PP + m] = w;
-        Ds[(4 * ty + i) * MF_PP + m] = ds;
+        const int m = tx + 16 * c;
+        const float w = __expf(z[i][c] - lses[m]);
+        Ps[(MF_RPT * ty + i) * MF_PP + m] = w;
+        Ds[(MF_RPT * ty + i) * MF_PP + m] = w > 0.f ? w * (dp[i][c] - deltas[m]) * bend[i][c] : 0.f;
       }
     __syncwarp();
     accumulate<DP>(Ps, Cs, ty, tx, dv);
@@ -438,10 +460,10 @@ masked_dkv_kernel(const MaskedParams p) {
     if (j + 1 < n * group) ask_q(j + 1);
   }
   // keys beyond the sequence are zero rows that may have been given scores where nothing is tested
-  float one[4], f[4];
+  float one[MF_RPT], f[MF_RPT];
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    one[i] = k0 + 4 * ty + i < s.len ? 1.f : 0.f;
+  for (int i = 0; i < MF_RPT; i++) {
+    one[i] = k0 + MF_RPT * ty + i < s.len ? 1.f : 0.f;
     f[i] = p.m.scale * one[i];
   }
   store_rows<DP>(p.o0, b, k0, hk, p.m.S, p.D, ty, tx, dk, f);
