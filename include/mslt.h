@@ -533,8 +533,9 @@ int mslt_op_qk_norm_rope_bwd(const mslt_qk_norm_desc* desc, void* d_scratch, siz
  * A query that sees no key gets ctx 0, lse -infinity and no gradient.  Query head h reads key head h / (heads / kv_heads).
  * Rows at or beyond a sequence's length take no part, whatever they hold (NaN too).
  * bf16: probabilities (relative to a power of two of the row's) are rounded to bf16 before the product with v, and the row
- * is divided by the sum of what was rounded.  `rest` (bf16, ctx's strides) receives what rounding took off ctx; given to the
- * backward call it makes the rows of the scores' gradient sum to zero also where the keys have much in common.
+ * is divided by the sum of what was rounded.  With `rest` (bf16, ctx's strides), as a training step calls it, the product
+ * also takes what that rounding took off, and `rest` receives what rounding took off ctx: given to the backward call it
+ * makes the rows of the scores' gradient sum to zero also where the keys have much in common.
  * Backward: the gradients of ctx by q, k and v from dctx, ctx, lse (and rest) of the forward call; dk and dv are summed over
  * the query heads that share them, in a fixed order.  The slopes are constants and have no gradient.
  */

@@ -1,20 +1,22 @@
-// Attention under masks in bf16 on the tensor cores, forward and backward, for head widths up to 128 (formulas: attn_masked.h).
-// The scores never reach memory.  Three kernels of one build: a block owns 128 rows of one head (queries in the
-// forward and for dQ, keys for dK and dV), a thread of its four softmax warps owns a row, and the loop runs over blocks
-// of 64 rows of the other side that the mask leaves:
+// Attention under masks in bf16 on the tensor cores, forward and backward, for head widths up to 128 (formulas: mslt.h).
+// The scores never reach memory.  Three kernels: a block owns 128 rows of one head at a time (queries in the forward and for
+// dQ, keys for dK and dV), and the loop runs over blocks of 64 or 128 rows of the other side that the mask leaves:
 //   forward  S = Q K^T                 P = 2^(S' - m)                               O += P V
 //   dQ       S = Q K^T, dP = dC V^T    dS = P (dP - delta) dz/ds                    dQ += dS K
 //   dK, dV   S^T = K Q^T, dP^T = V dC^T, the same transposed                        dV += P^T dC, dK += dS^T Q
 // P and dS are the A operand of the second product and never leave tensor memory: they are written over the scores they
-// come from.  dQ and dK/dV are two launches that form S and dP twice (7 products in the place of 5): in return no sum
+// come from.  dQ and dK, dV are two launches that form S and dP twice (7 products in the place of 5): in return no sum
 // crosses blocks, so every run gives the same bits and nothing is added by atomics.
-//   warp 0: TMA producer; warp 1: one thread issues the products; the others: softmax, a thread a row (forward) or half a
-//   row's columns (backward, where the rows' sums are known)
-// What bounds it: the exponential unit takes 512 cycles for 128 x 64 scores, the forward's products 256 (heads of 64), and
-// around both lies a chain of waits and tensor-memory reads of some 1500 cycles a loop block.  So blocks are small and many
-// share an SM, one working while the others wait: heads of 64, four forward blocks (128 columns of tensor memory, 80
-// registers, scores read twice in the place of 64 registers) and two backward blocks of eight softmax warps.  Measured
-// with two forward blocks of double-buffered scores: a loop block took 1660 cycles of a block, 1120 of the SM.
+//   warp 0: TMA producer; warp 1: one thread issues the products; the others: softmax, a thread a row (forward: 4 warps) or 32
+//   (16) columns of a row (backward, where the rows' sums are known: 16 warps)
+// What bounds it.  The exponential unit takes 1024 cycles for 128 x 128 scores, the products 512 in the forward, 768 for dQ and
+// 1024 for dK and dV at heads of 64 (twice that at 128).  Around both lies the chain of a step: waits of 150 cycles, reads of
+// tensor memory of 100, dependent instructions of three or four warps a scheduler.  So many warps share an SM: heads of 64, four
+// forward blocks (128 columns of tensor memory and 80 registers each), sixteen softmax warps of one backward block.
+// Measured with 37 tiles a head x 16 heads, all SMs full, cycles of an SM for 128 x 128 scores: forward 1690 (exponential unit
+// 59 % busy), dQ 2150 (52 %), dK and dV 2700 (42 %).  Tried on it: two forward blocks of double-buffered scores 2240; scores
+// held in registers by three blocks 2330; a quarter to a half of the backward's exponentials by polynomial 3 to 12 % slower;
+// eight backward softmax warps of 64 columns 3 % slower; polls with a suspend time: level.
 //
 // Which blocks a row tile visits is worked out once, at its start, from positions, length, prefix and the least and
 // greatest document of either side: left out, whole, or with pairs to test.  Documents may be in any order; where they
@@ -438,11 +440,24 @@ template <int DP> struct FwdShape {
   static constexpr int SMEM = Q_BYTES + 2 * STAGES * KV_BYTES;
 };
 
+// x less the two bf16 of h, as bf16
+__device__ __forceinline__ uint32_t less_bf16(float2 x, uint32_t h) {
+  float lo, hi;
+  asm("{\n\t.reg .b16 l, h;\n\t"
+      "mov.b32 {l, h}, %2;\n\t"
+      "sub.f32.bf16 %0, l, %3;\n\t"
+      "sub.f32.bf16 %1, h, %4;\n\t}"
+      : "=f"(lo), "=f"(hi)
+      : "r"(h), "f"(x.x), "f"(x.y));
+  return pack2(-lo, -hi);
+}
+
 // Probabilities of 32 columns: 2^(exponent - base), rounded to bf16; sums of the rounded and of the unrounded ones.  see: the
-// columns that count, all of them where there is nothing to test.
-template <int kForm>
+// columns that count, all of them where there is nothing to test.  kRest: what the rounding took off follows the rounded ones
+// (and their sum is not needed).
+template <int kForm, bool kRest>
 __device__ __forceinline__ void probabilities(const Form& f, const Piece& pc, const uint32_t (&s)[32], bool test, uint32_t see,
-                                              float base, uint32_t (&pk)[16], float2& sum, float2& exact) {
+                                              float base, uint32_t (&pk)[16], uint32_t (&rest)[16], float2& sum, float2& exact) {
   choose_way<kForm>(f, pc, test, [&](auto way) {
     typedef decltype(way) Wy;
 #pragma unroll
@@ -456,7 +471,8 @@ __device__ __forceinline__ void probabilities(const Form& f, const Piece& pc, co
       e.y = ex2(e.y);
       pk[c / 2] = pack2(e.x, e.y);
       exact = __fadd2_rn(exact, e);
-      add_bf16(sum, pk[c / 2]);
+      if (kRest) rest[c / 2] = less_bf16(e, pk[c / 2]);
+      else add_bf16(sum, pk[c / 2]);
     }
   });
 }
@@ -620,7 +636,8 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
         fine = landed(vfull, j) && mbar_wait(smem_u32(&pready[j & 1]), j >> 1 & 1, abort_flag, p.status);
         if (!fine) break;
         tc_fence_after();
-        product_ts<AF_COLS, 2>(tmem + Sh::O_COL, tmem + (j % SB) * 64, 16, smem_u32(Vs + st * Sh::KV_BYTES), id_o, j > j0);
+        product_ts<AF_COLS, 2>(tmem + Sh::O_COL, tmem + (j % SB) * 64, 32, smem_u32(Vs + st * Sh::KV_BYTES), id_o, j > j0);
+        if (p.rest) product_ts<AF_COLS, 2>(tmem + Sh::O_COL, tmem + (j % SB) * 64 + 16, 32, smem_u32(Vs + st * Sh::KV_BYTES), id_o, 1);
         if (SB == 2) tc_commit(smem_u32(&odone[j & 1]));
         // one buffer: the probabilities lie in it until the product with V, issued before, has read them
         if (SB == 1 && j + 1 < j1) scores(j + 1);
@@ -691,14 +708,24 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
           settled = go == 0 && __all_sync(0xffffffffu, top != -INFINITY);
         }
         const float base = top == -INFINITY ? 0.f : top;
-        // The probabilities of a half take 16 columns of the scores that were read for the half.
+        // The probabilities of a half take 16 of the 32 columns of scores that were read for it.  A training step's context is
+        // formed from more than bf16 holds of them: what their rounding takes off goes to the other 16 columns and
+        // through a second product.  The backward's delta = dC . C follows the probabilities to 2^-16 then, and rows of the
+        // scores' gradient sum to zero; with the rounded ones alone dQ was off by 2.6e-3 of its norm where the roundings of
+        // dS and dQ themselves make 2.4e-3.
 #pragma unroll
         for (int half = 0; half < 2; half++) {
           tc_ld32_issue(tS + 32 * half, a);
           tc_ld32_wait(a);
-          uint32_t pk[16];
-          probabilities<kForm>(f, piece_of<kForm>(f, r, c0 + 32 * half, a), a, test, see[half], base, pk, sum, exact);
-          tc_st16(tS + 16 * half, pk);
+          uint32_t pk[16], rest[16];
+          const Piece pc = piece_of<kForm>(f, r, c0 + 32 * half, a);
+          if (p.rest) {
+            probabilities<kForm, true>(f, pc, a, test, see[half], base, pk, rest, sum, exact);
+            tc_st16(tS + 32 * half + 16, rest);
+          } else {
+            probabilities<kForm, false>(f, pc, a, test, see[half], base, pk, rest, sum, exact);
+          }
+          tc_st16(tS + 32 * half, pk);
         }
         tc_st_wait();
         if (test && s.len < c0 + AF_COLS) {
@@ -719,7 +746,7 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 
   if (warp >= 2 && ok) {
     tc_fence_after();
-    const float total = sum.x + sum.y;
+    const float total = p.rest ? exact.x + exact.y : sum.x + sum.y;
     const bool empty = r >= s.len || !(total > 0.f);
     const long long at = b * p.o0.batch + r * p.o0.row + h * p.o0.head;
     store_row(trow + Sh::O_COL, p.o0.p + at, p.rest ? p.rest + at : nullptr, empty ? 0.f : 1.f / total, empty, n > 0, r < p.m.S, p.wide, 0, DP,

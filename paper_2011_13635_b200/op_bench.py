@@ -27,7 +27,7 @@ def main(argv=None, emit=print):
     ap.add_argument("--batch", type=int, default=128)
     ap.add_argument("--dtype", default="bf16", choices=["bf16", "fp32"])
     ap.add_argument("--iters", type=int, default=40)
-    ap.add_argument("--only", default="", help="comma-separated kernel groups: ln, colsum, softmax, attention, ce")
+    ap.add_argument("--only", default="", help="comma-separated kernel groups: ln, colsum, softmax, attention, ce, rotary, masked")
     a = ap.parse_args(argv)
     only = set(x for x in a.only.split(",") if x)
     want = lambda group: not only or group in only
@@ -81,6 +81,46 @@ def main(argv=None, emit=print):
         if int(status.item()) != 0:
             raise RuntimeError("the attention kernel reported a wait that ran out")
         del qs, ctx, probs
+    if want("rotary"):
+        # queries and keys in the fused projection's rows: rotation; norm and rotation; their backward
+        A = a.heads
+        xs = rotation((T, 3 * A, 64), tdt)
+        heads = [x[:, :2 * A] for x in xs]
+        y, dy = torch.empty((T, 2 * A, 64), device="cuda", dtype=tdt), torch.randn((T, 2 * A, 64), device="cuda").to(tdt)
+        gain, dgain = torch.ones((2, 64), device="cuda"), torch.empty((2, 64), device="cuda")
+        turns = torch.from_numpy(Bd.mslt_rope_turns(64)[0].view("int64")).cuda()
+        scratch = torch.empty(Bd.mslt_op_qk_norm_rope_bwd_scratch_bytes(T, 2 * A, 64), dtype=torch.uint8, device="cuda")
+        n = T * 2 * A * 64 * E
+        run("rope", 2 * n, lambda i: Bd.mslt_op_rope(heads[i], y, turns, st, seq=a.seq, sync=False), len(xs))
+        run("qk_norm_rope", 2 * n,
+            lambda i: Bd.mslt_op_qk_norm_rope(heads[i], y, gain, turns, A, 1e-6, st, seq=a.seq, sync=False), len(xs))
+        run("qk_norm_rope_backward", 3 * n,
+            lambda i: Bd.mslt_op_qk_norm_rope_bwd(dy, heads[i], y, gain, dgain, turns, A, 1e-6, scratch, st, seq=a.seq, sync=False),
+            len(xs))
+        del xs, heads, y, dy
+    if want("masked"):
+        # attention under a causal mask, as a training step and as an evaluation call it
+        B, S, A = a.batch, a.seq, a.heads
+        qs = [x.view(B, S, 3 * A, 64) for x in rotation((B * S, 3 * A * 64), tdt)]
+        parts = [(x[:, :, :A], x[:, :, A:2 * A], x[:, :, 2 * A:]) for x in qs]
+        ctx, lse = torch.empty((B, S, A, 64), device="cuda", dtype=tdt), torch.empty((B, A, S), device="cuda")
+        rest = torch.empty_like(ctx) if a.dtype == "bf16" else None
+        grads = [torch.empty_like(ctx) for _ in range(3)]
+        dctx = torch.randn(ctx.shape, device="cuda").to(tdt)
+        scratch = torch.empty(Bd.mslt_op_attention_masked_bwd_scratch_bytes(B, S, A), dtype=torch.uint8, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        n = B * S * A * 64 * E
+        run("attention_masked", 4 * n,
+            lambda i: Bd.mslt_op_attention_masked(*parts[i], ctx, None, 0.125, status, st, causal=True, sync=False), len(qs))
+        run("attention_masked_training", (5 if rest is not None else 4) * n,
+            lambda i: Bd.mslt_op_attention_masked(*parts[i], ctx, lse, 0.125, status, st, causal=True, rest=rest, sync=False), len(qs))
+        # the forward's results belong to the last buffer: the others give the same work, not gradients
+        run("attention_masked_backward", (9 if rest is not None else 8) * n,
+            lambda i: Bd.mslt_op_attention_masked_bwd(*parts[i], ctx, lse, dctx, *grads, scratch, 0.125, status, st, causal=True,
+                                                      rest=rest, sync=False), len(qs))
+        if int(status.item()) != 0:
+            raise RuntimeError("the attention kernel reported a wait that ran out")
+        del qs, parts, ctx, grads
     if not (want("ln") or want("colsum") or want("softmax") or want("ce")):
         return records
     gamma = torch.ones(H, device="cuda"); beta = torch.zeros(H, device="cuda")
