@@ -471,7 +471,7 @@ typedef struct {
   const void* x;                  /* device; element (t, h, e) at x + t * x_row + h * x_head + e         */
   int64_t x_row, x_head;          /* elements; multiples of 16 bytes, as is the address                  */
   void* y;                        /* device, likewise                                                    */
-  int64_t y_row, y_head;
+  int64_t y_row, y_head;          /* at least head_dim                                                   */
   const int32_t* positions;       /* device [rows], any int32; NULL: row t is at position t % seq        */
   int32_t seq;                    /* rows of a sequence, used where positions is NULL                    */
   int32_t rot_dim;                /* a multiple of 8 in [8, head_dim]; the normalising calls also take 0 */
@@ -514,7 +514,7 @@ typedef struct {
   const void* dy;        /* backward: device, element (t, h, e) at dy + t * dy_row + h * dy_head + e */
   int64_t dy_row, dy_head;
   void* dx;
-  int64_t dx_row, dx_head;
+  int64_t dx_row, dx_head;   /* at least head_dim */
   float* dgain;          /* backward: device [2, head_dim], 16-byte aligned */
   float* dbias;          /* backward: device [2, head_dim] or NULL */
 } mslt_qk_norm_desc;
@@ -531,7 +531,8 @@ int mslt_op_qk_norm_rope_bwd(const mslt_qk_norm_desc* desc, void* d_scratch, siz
  *                               j <= i or j < prefix  (causal; without prefix: j <= i)
  *     ctx_i = sum_j softmax_j(z_ij) v_j over the keys that query i sees, lse_i = ln sum_j e^(z_ij)
  * A query that sees no key gets ctx 0, lse -infinity and no gradient.  Query head h reads key head h / (heads / kv_heads).
- * Rows at or beyond a sequence's length take no part, whatever they hold (NaN too).
+ * Rows at or beyond a sequence's length take no part, whatever they hold (NaN too).  NaN in another row of q or k
+ * reaches the outputs that depend on it, and may reach gradients of its sequence that do not.
  * bf16: probabilities (relative to a power of two of the row's) are rounded to bf16 before the product with v, and the row
  * is divided by the sum of what was rounded.  With `rest` (bf16, ctx's strides), as a training step calls it, the product
  * also takes what that rounding took off, and `rest` receives what rounding took off ctx: given to the backward call it
@@ -541,16 +542,18 @@ int mslt_op_qk_norm_rope_bwd(const mslt_qk_norm_desc* desc, void* d_scratch, siz
  */
 typedef struct {
   void* data;                 /* device; element (b, i, h, e) at data + b * batch + i * row + h * head + e */
-  int64_t batch, row, head;   /* elements; multiples of 16 bytes, as is the address (an extent of 1: not used) */
+  int64_t batch, row, head;   /* elements; multiples of 16 bytes, as is the address (an extent of 1: not used); above 0, and
+                                 of what a call writes at least head_dim */
 } mslt_heads;
 typedef struct {
   int32_t dtype;                                  /* 0: fp32, 1: bf16                          */
-  int32_t B, S, heads, kv_heads, head_dim;        /* head_dim a multiple of 8, <= 128; heads a multiple of kv_heads; S <= 131072 */
+  int32_t B, S, heads, kv_heads, head_dim;        /* head_dim a multiple of 8, <= 128; heads a multiple of kv_heads;
+                                                     S <= 131072, B heads S <= 2^30 */
   mslt_heads q, k, v, ctx;                        /* inputs and output of the forward call      */
   void* rest;                                     /* dtype 1: ctx's layout, or NULL              */
   float* lse;                                     /* device [B, heads, S]; forward: may be NULL  */
   mslt_heads dctx, dq, dk, dv;                    /* backward call                               */
-  float scale, cap;                               /* cap 0: none                                 */
+  float scale, cap;                               /* cap 0: none; else cap and |scale| / cap in [2^-64, 2^64] (scale 0 too) */
   const float* slopes;                            /* device [heads] or NULL                      */
   int32_t causal;
   const int32_t* prefix;                          /* device [B] or NULL; needs causal            */

@@ -24,13 +24,17 @@ mslt_attention_desc tidy(const mslt_attention_desc& d) {
   return t;
 }
 
-// h: tidied
-int check_heads(const char* what, const char* name, const mslt_heads& h, int dtype) {
-  const int unit = dtype == 1 ? 8 : 4;
+// h: tidied.  An input's stride of 0 has no tensor map; an output's below a head's width would have blocks write to one place.
+int check_heads(const char* what, const char* name, const mslt_heads& h, const mslt_attention_desc& d, int heads, bool output) {
+  const int unit = d.dtype == 1 ? 8 : 4;
   if (!h.data) return op_refuse(MSLT_ERR_ARG, "%s: %s is null", what, name);
   if ((uintptr_t)h.data & 15) return op_refuse(MSLT_ERR_ARG, "%s: %s must be 16-byte aligned", what, name);
   if (h.batch < 0 || h.row < 0 || h.head < 0 || h.batch % unit || h.row % unit || h.head % unit)
     return op_refuse(MSLT_ERR_ARG, "%s: strides of %s must be multiples of 16 bytes", what, name);
+  const int64_t least = output ? d.head_dim : 1;
+  if ((d.B > 1 && h.batch < least) || (d.S > 1 && h.row < least) || (heads > 1 && h.head < least))
+    return op_refuse(MSLT_ERR_ARG, output ? "%s: strides of %s must be at least head_dim" : "%s: %s must not be broadcast by a stride of 0", what,
+                     name);
   return 0;
 }
 
@@ -41,16 +45,20 @@ int check_attention(const char* what, const mslt_attention_desc* d, const int32_
     return op_refuse(MSLT_ERR_ARG, "%s: needs B, S, heads >= 1 and heads a multiple of kv_heads", what);
   if (d->head_dim < 8 || d->head_dim > 128 || d->head_dim % 8)
     return op_refuse(MSLT_ERR_ARG, "%s: head_dim must be a multiple of 8 in [8, 128]", what);
-  if (d->S > 131072 || (int64_t)d->B * d->heads * d->S > 0x7fffffffll)
-    return op_refuse(MSLT_ERR_SIZE, "%s: at most 131072 rows a sequence and 2^31 - 1 rows of all heads", what);
+  if (d->S > 131072 || (int64_t)d->B * d->heads * d->S > (1ll << 30))
+    return op_refuse(MSLT_ERR_SIZE, "%s: at most 131072 rows a sequence and 2^30 rows of all heads", what);
   if (!isfinite(d->scale) || !isfinite(d->cap) || d->cap < 0)
     return op_refuse(MSLT_ERR_ARG, "%s: scale and cap must be finite, cap not negative", what);
+  // 2^64 either way: products of the cap, its inverse and the scale stay within fp32
+  const float most = 0x1p64f, least = 0x1p-64f, by = fabsf(d->scale) / (d->cap > 0 ? d->cap : 1.f);
+  if (d->cap > 0 && (d->cap > most || d->cap < least || by > most || (d->scale != 0 && by < least)))
+    return op_refuse(MSLT_ERR_ARG, "%s: cap and scale / cap must be in [2^-64, 2^64]", what);
   if (d->prefix && !d->causal) return op_refuse(MSLT_ERR_ARG, "%s: a prefix needs causal", what);
   if (d->dtype == 0 && d->rest) return op_refuse(MSLT_ERR_ARG, "%s: rest is for dtype 1", what);
   if ((uintptr_t)d->rest & 15) return op_refuse(MSLT_ERR_ARG, "%s: rest must be 16-byte aligned", what);
   int rc = 0;
-  if ((rc = check_heads(what, "q", d->q, d->dtype)) || (rc = check_heads(what, "k", d->k, d->dtype)) ||
-      (rc = check_heads(what, "v", d->v, d->dtype)) || (rc = check_heads(what, "ctx", d->ctx, d->dtype)))
+  if ((rc = check_heads(what, "q", d->q, *d, d->heads, false)) || (rc = check_heads(what, "k", d->k, *d, d->kv_heads, false)) ||
+      (rc = check_heads(what, "v", d->v, *d, d->kv_heads, false)) || (rc = check_heads(what, "ctx", d->ctx, *d, d->heads, true)))
     return rc;
   return 0;
 }
@@ -96,8 +104,10 @@ int mslt_op_attention_masked_bwd(const mslt_attention_desc* caller, void* d_scra
   const mslt_attention_desc given = tidy(*caller), *desc = &given;
   int rc = check_attention(what, desc, d_status);
   if (rc) return rc;
-  if ((rc = check_heads(what, "dctx", desc->dctx, desc->dtype)) || (rc = check_heads(what, "dq", desc->dq, desc->dtype)) ||
-      (rc = check_heads(what, "dk", desc->dk, desc->dtype)) || (rc = check_heads(what, "dv", desc->dv, desc->dtype)))
+  if ((rc = check_heads(what, "dctx", desc->dctx, *desc, desc->heads, false)) ||
+      (rc = check_heads(what, "dq", desc->dq, *desc, desc->heads, true)) ||
+      (rc = check_heads(what, "dk", desc->dk, *desc, desc->kv_heads, true)) ||
+      (rc = check_heads(what, "dv", desc->dv, *desc, desc->kv_heads, true)))
     return rc;
   if (!desc->lse) return op_refuse(MSLT_ERR_ARG, "%s: lse is null", what);
   const size_t need = mslt_op_attention_masked_bwd_scratch_bytes(desc->B, desc->S, desc->heads);

@@ -1,7 +1,7 @@
 // Attention under masks in fp32, forward and backward, on the CUDA cores (a tolerance of 1e-4 and less rules the
 // tensor cores' formats out, and the split of operands into bf16 planes costs more than it gains on scores that are
 // used once).  The scores never reach memory:
-//   forward   a block of 64 queries walks over the key tiles that its mask leaves, with the running maximum and sum
+//   forward   a block of 32 queries walks over the key tiles that its mask leaves, with the running maximum and sum
 //   backward  P = e^(z - lse), dS = P (dP - delta) dz/ds, delta = rowsum(dC C); dQ = scale dS K by blocks of queries,
 //             dK = scale dS^T Q and dV = P^T dC by blocks of keys, over all query heads that share them
 // A block owns 32 rows, 128 threads hold 4 x 4 scores each, then 4 rows x 4 (8) columns of the accumulators, as packed
@@ -277,7 +277,7 @@ masked_fwd_kernel(const MaskedParams p) {
   float f[MF_RPT];
 #pragma unroll
   for (int i = 0; i < MF_RPT; i++) {
-    f[i] = sum[i] > 0.f ? 1.f / sum[i] : 0.f;
+    f[i] = sum[i] == 0.f ? 0.f : 1.f / sum[i];
     const int r = q0 + MF_RPT * ty + i;
     const bool dead = r >= s.len;  // its row of Q is zero and may have been given scores where nothing is tested
     if (dead) f[i] = 0.f;
@@ -366,7 +366,7 @@ masked_dq_kernel(const MaskedParams p) {
 #pragma unroll
       for (int c = 0; c < 4; c++) {
         const float w = __expf(z[i][c] - lse[i]);
-        Ps[(MF_RPT * ty + i) * MF_PP + tx + 16 * c] = w > 0.f ? w * (dp[i][c] - delta[i]) * bend[i][c] : 0.f;
+        Ps[(MF_RPT * ty + i) * MF_PP + tx + 16 * c] = w == 0.f ? 0.f : w * (dp[i][c] - delta[i]) * bend[i][c];
       }
     __syncwarp();  // the scores of a thread's rows are its half warp's
     accumulate<DP>(Ps, Ks, ty, tx, acc);
@@ -449,7 +449,7 @@ masked_dkv_kernel(const MaskedParams p) {
         const int m = tx + 16 * c;
         const float w = __expf(z[i][c] - lses[m]);
         Ps[(MF_RPT * ty + i) * MF_PP + m] = w;
-        Ds[(MF_RPT * ty + i) * MF_PP + m] = w > 0.f ? w * (dp[i][c] - deltas[m]) * bend[i][c] : 0.f;
+        Ds[(MF_RPT * ty + i) * MF_PP + m] = w == 0.f ? 0.f : w * (dp[i][c] - deltas[m]) * bend[i][c];
       }
     __syncwarp();
     accumulate<DP>(Ps, Cs, ty, tx, dv);

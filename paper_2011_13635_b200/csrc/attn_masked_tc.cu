@@ -21,7 +21,7 @@
 // Which blocks a row tile visits is worked out once, at its start, from positions, length, prefix and the least and
 // greatest document of either side: left out, whole, or with pairs to test.  Documents may be in any order; where they
 // are sorted, as in a packed batch, exactly the blocks that hold a common document are visited.  Only blocks with pairs
-// to test pay for it: a 64-bit word per row says which pairs count.
+// to test pay for it: a 32-bit word for 32 columns of a row says which pairs count.
 // Rows beyond a sequence may hold anything: those of the row tile give rows that are not stored, those of the other
 // side are cleared in shared memory (zero times NaN is NaN) by the softmax warps before the product that contracts over
 // them.
@@ -240,13 +240,13 @@ __device__ __forceinline__ Form form_of(const AttnMask& m, int h) {
     f.cap2 = m.cap * LOG2E;
     f.inv_cap2 = 1.f / f.cap2;
     f.z_by = k * (2.f * LOG2E);  // 2^(s z_by) = e^(2 z / cap)
-    f.small = 0.375f / fabsf(k);
     float by = f.cap2 * k;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
       f.b[i] = kT[i] * by;
       by *= k * k;
     }
+    f.small = isinf(f.b[3]) ? -1.f : 0.375f / fabsf(k);  // caps far below the scale: no polynomial
   }
   return f;
 }
@@ -314,8 +314,6 @@ __device__ __forceinline__ float2 exponents(const Form& f, const Piece& p, float
 }
 
 // ---- pieces of the roles ----------------------------------------------------------------------------------
-
-struct Ring { uint64_t *full, *empty; };
 
 __device__ __forceinline__ uint32_t addr16(uint32_t a) { return (a & 0x3FFFFu) >> 4; }
 
@@ -747,7 +745,7 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
   if (warp >= 2 && ok) {
     tc_fence_after();
     const float total = p.rest ? exact.x + exact.y : sum.x + sum.y;
-    const bool empty = r >= s.len || !(total > 0.f);
+    const bool empty = r >= s.len || total == 0.f;  // NaN is not
     const long long at = b * p.o0.batch + r * p.o0.row + h * p.o0.head;
     store_row(trow + Sh::O_COL, p.o0.p + at, p.rest ? p.rest + at : nullptr, empty ? 0.f : 1.f / total, empty, n > 0, r < p.m.S, p.wide, 0, DP,
               p.D);

@@ -392,7 +392,7 @@ RotaryLaunch run_rotary(const mslt_rope_desc& d, RotaryParams& p, int sms, cudaS
 }
 
 // the strides of a single row and of a single head are not used
-int check_strided(const char* what, const char* name, const mslt_rope_desc& d, const void* ptr, int64_t row, int64_t head) {
+int check_strided(const char* what, const char* name, const mslt_rope_desc& d, const void* ptr, int64_t row, int64_t head, bool output) {
   const int dtype = d.dtype;
   if (d.rows == 1) row = 0;
   if (d.heads == 1) head = 0;
@@ -401,6 +401,8 @@ int check_strided(const char* what, const char* name, const mslt_rope_desc& d, c
   if ((uintptr_t)ptr & 15) return op_refuse(MSLT_ERR_ARG, "%s: %s must be 16-byte aligned", what, name);
   if (row % unit || head % unit || row < 0 || head < 0)
     return op_refuse(MSLT_ERR_ARG, "%s: strides of %s must be multiples of 16 bytes", what, name);
+  if (output && ((d.rows > 1 && row < d.head_dim) || (d.heads > 1 && head < d.head_dim)))
+    return op_refuse(MSLT_ERR_ARG, "%s: strides of %s must be at least head_dim", what, name);
   return 0;
 }
 
@@ -417,7 +419,7 @@ int check_rope(const char* what, const mslt_rope_desc* d, int rot_min) {
     return op_refuse(MSLT_ERR_ARG, "%s: turns must be 16-byte aligned and not null", what);
   if (!d->positions && d->seq < 1) return op_refuse(MSLT_ERR_ARG, "%s: without positions seq must be >= 1", what);
   if (!isfinite(d->magnitude)) return op_refuse(MSLT_ERR_ARG, "%s: magnitude must be finite", what);
-  return check_strided(what, "x", *d, d->x, d->x_row, d->x_head);
+  return check_strided(what, "x", *d, d->x, d->x_row, d->x_head, false);
 }
 
 void fill_rope(const mslt_rope_desc& d, RotaryParams& p) {
@@ -487,7 +489,7 @@ int mslt_rope_turns(int32_t rot_dim, double base, int32_t scaling, double factor
 int mslt_op_rope(const mslt_rope_desc* desc, void* cuda_stream, int32_t sync) {
   int rc = check_rope("rope", desc, 8);
   if (rc) return rc;
-  rc = check_strided("rope", "y", *desc, desc->y, desc->y_row, desc->y_head);
+  rc = check_strided("rope", "y", *desc, desc->y, desc->y_row, desc->y_head, true);
   if (rc) return rc;
   int sms = 0;
   if ((rc = op_need_device()) || (rc = sm_count(&sms))) return rc;
@@ -500,7 +502,7 @@ int mslt_op_rope(const mslt_rope_desc* desc, void* cuda_stream, int32_t sync) {
 int mslt_op_qk_norm_rope(const mslt_qk_norm_desc* desc, void* cuda_stream, int32_t sync) {
   int rc = check_norm("qk_norm_rope", desc);
   if (rc) return rc;
-  rc = check_strided("qk_norm_rope", "y", desc->rope, desc->rope.y, desc->rope.y_row, desc->rope.y_head);
+  rc = check_strided("qk_norm_rope", "y", desc->rope, desc->rope.y, desc->rope.y_row, desc->rope.y_head, true);
   if (rc) return rc;
   int sms = 0;
   if ((rc = op_need_device()) || (rc = sm_count(&sms))) return rc;
@@ -522,8 +524,8 @@ int mslt_op_qk_norm_rope_bwd(const mslt_qk_norm_desc* desc, void* d_scratch, siz
   const char* what = "qk_norm_rope_bwd";
   int rc = check_norm(what, desc);
   if (rc) return rc;
-  if ((rc = check_strided(what, "dy", desc->rope, desc->dy, desc->dy_row, desc->dy_head))) return rc;
-  if ((rc = check_strided(what, "dx", desc->rope, desc->dx, desc->dx_row, desc->dx_head))) return rc;
+  if ((rc = check_strided(what, "dy", desc->rope, desc->dy, desc->dy_row, desc->dy_head, false))) return rc;
+  if ((rc = check_strided(what, "dx", desc->rope, desc->dx, desc->dx_row, desc->dx_head, true))) return rc;
   if (!desc->dgain) return op_refuse(MSLT_ERR_ARG, "%s: dgain is null", what);
   const size_t need = mslt_op_qk_norm_rope_bwd_scratch_bytes(desc->rope.rows, desc->rope.heads, desc->rope.head_dim);
   if (!d_scratch || scratch_bytes < need || ((uintptr_t)d_scratch & 15))

@@ -524,6 +524,64 @@ def test_refusals_before_any_device():
     assert B.lib.mslt_op_attention_masked(B.C.byref(desc(B)), None, None, 1) == -1
 
 
+def test_refusals_of_strides_and_ranges():
+    """Broadcast inputs, outputs whose elements share memory, sizes past the row counters, caps that fp32 cannot turn over."""
+    from paper_2011_13635_b200 import binding as B
+    fwd = lambda d: B.lib.mslt_op_attention_masked(B.C.byref(d), 4096, None, 1)                             # noqa: E731
+    size = B.mslt_op_attention_masked_bwd_scratch_bytes(2, 128, 4)
+    bwd = lambda d: B.lib.mslt_op_attention_masked_bwd(B.C.byref(d), 4096, size, 4096, None, 1)              # noqa: E731
+    for dtype in (0, 1):
+        for f in ("batch", "row", "head"):
+            for t in ("q", "k", "v", "ctx"):
+                assert fwd(desc(B, dtype=dtype, **{f"{t}.{f}": 0})) == -1 and bwd(desc(B, dtype=dtype, **{f"{t}.{f}": 0})) == -1, (t, f)
+            for t in ("dctx", "dq", "dk", "dv"):
+                assert bwd(desc(B, dtype=dtype, **{f"{t}.{f}": 0})) == -1, (t, f)
+            for t in ("dq", "dk", "dv"):
+                assert bwd(desc(B, dtype=dtype, **{f"{t}.{f}": 56})) == -1, (t, f)
+            assert fwd(desc(B, dtype=dtype, **{f"ctx.{f}": 56})) == -1, f
+        for change in (dict(cap=1e-20), dict(cap=1e20), dict(cap=1e-3, scale=1e17), dict(cap=1.0, scale=1e-20), dict(cap=1.0, scale=-1e20)):
+            assert fwd(desc(B, dtype=dtype, **change)) == -1, change
+        assert fwd(desc(B, dtype=dtype, B=1 << 28, S=1, heads=8)) == -2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("kw", [dict(cap=1e-12), dict(cap=1e6), dict(cap=1e-12, slopes=True), dict(cap=5.0, zero_scale=True)], ids=str)
+def test_caps_far_from_the_scores(dtype, kw):
+    """Far below, every score but those of zero queries is at its cap; far above, the cap does nothing; scale 0: all alike."""
+    kw = dict(kw)
+    zero = kw.pop("zero_scale", False)
+    s = make(dtype, 1, 200, 2, 1, 64, causal=True, **kw)
+    s["q"][:, 5:9] = 0
+    if zero:
+        s["scale"] = 0.0
+    check(s, run(s))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("kw", [{}, dict(slopes=True), dict(cap=20.0)], ids=str)
+def test_nan_that_is_seen_comes_through(dtype, dim, kw):
+    """A NaN in a query or a key is not passed over as a row that sees nothing."""
+    import torch
+    for name in ("q", "k"):
+        s = make(dtype, 2, 300, 2, 2, dim, causal=True, **kw)
+        s[name][0, 150, 1, 3] = float("nan")
+        out = run(s)
+        bad = torch.isnan(out["ctx"]).all(-1)[0, :, 1]
+        want = torch.zeros(300, dtype=torch.bool, device="cuda")
+        want[150 if name == "q" else slice(150, None)] = True
+        if name == "q":
+            want[151:] = False
+        assert torch.equal(bad, want) and torch.equal(torch.isnan(out["ctx"])[0, :, 1].any(-1), want)
+        assert torch.equal(torch.isnan(out["lse"])[0, 1], want)
+        assert torch.isnan(out["dq"][0, :, 1][want]).all()
+        assert torch.isnan(out["dk"][0, :150, 1]).all() and torch.isnan(out["dv"][0, :150, 1]).all()
+        for k in ("ctx", "dq", "dk", "dv"):
+            assert not torch.isnan(out[k][1]).any() and not torch.isnan(out[k][0, :, 0]).any(), k
+
+
 @pytest.mark.gpu
 def test_binding_refusals():
     import torch

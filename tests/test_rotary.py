@@ -120,6 +120,21 @@ def test_refusals_before_any_device():
         assert rc(lambda d: B.lib.mslt_op_qk_norm_rope_bwd(B.C.byref(d), at, n, None, 1), {}) == -2
 
 
+def test_refusals_of_outputs_that_share_memory():
+    from paper_2011_13635_b200 import binding as B
+    good = dict(dtype=1, rows=4, heads=2, head_dim=64, x=4096, x_row=128, x_head=64, y=8192, y_row=128, y_head=64, seq=4, rot_dim=64,
+                turns=16384, magnitude=1.0)
+    size = B.mslt_op_qk_norm_rope_bwd_scratch_bytes(4, 2, 64)
+    for field in ("row", "head"):
+        for stride in (0, 56):
+            d = B.RopeDesc(**dict(good, **{f"y_{field}": stride}))
+            n = B.QkNormDesc(rope=d, q_heads=1, eps=1e-6, gain=32768)
+            assert B.lib.mslt_op_rope(B.C.byref(d), None, 1) == -1 and B.lib.mslt_op_qk_norm_rope(B.C.byref(n), None, 1) == -1
+            n = B.QkNormDesc(rope=B.RopeDesc(**good), q_heads=1, eps=1e-6, gain=32768, dgain=32768,
+                             **dict(dict(dy=4096, dy_row=128, dy_head=64, dx=4096, dx_row=128, dx_head=64), **{f"dx_{field}": stride}))
+            assert B.lib.mslt_op_qk_norm_rope_bwd(B.C.byref(n), 65536, size, None, 1) == -1
+
+
 CASES = [  # dtype, rows, heads, dim, rot, interleaved
     ("bf16", 1, 1, 64, 64, False), ("bf16", 5, 3, 64, 64, True), ("bf16", 33, 24, 64, 32, False), ("bf16", 700, 7, 128, 128, False),
     ("bf16", 9, 5, 96, 24, False), ("bf16", 13, 2, 8, 8, False), ("bf16", 13, 2, 72, 72, False), ("bf16", 64, 9, 40, 40, True),
