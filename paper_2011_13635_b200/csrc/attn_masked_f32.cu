@@ -3,10 +3,13 @@
 // used once).  The scores never reach memory:
 //   forward   a block of 32 queries walks over the key tiles that its mask leaves, with the running maximum and sum
 //   backward  P = e^(z - lse), dS = P (dP - delta) dz/ds, delta = rowsum(dC C); dQ = scale dS K by blocks of queries,
-//             dK = scale dS^T Q and dV = P^T dC by blocks of keys, over all query heads that share them
+//             dK = scale dS^T Q and dV = P^T dC by blocks of keys, over all query heads that share them, in one launch
 // A block owns 32 rows, 128 threads hold 4 x 4 scores each, then 4 rows x 4 (8) columns of the accumulators, as packed
 // multiply-adds.  32 rows and not 64 because full precision is used on small batches, whose blocks have to fill the device:
-// 2 x 12 heads x 509 keys in 3 documents, forward | backward, 81 | 264 us with 64 rows and plain loads, 65 | 165 us so.  The
+// 2 x 12 heads x 509 keys in 3 documents, forward | backward, 81 | 264 us with 64 rows and plain loads, 65 | 165 us with 32 and
+// two launches for the backward, 65 | 132 us so.  What bounds it: where the device is full (4 x 12 x 512) half of the
+// multiply-adds' issue slots (110 | 311 us of 46 | 140), on small batches the longest blocks' steps one after the other, 3 us
+// each for a block alone on its SM (5500 cycles, 2050 of them multiply-adds).  The
 // other side's tiles of 64 rows are asked for by asynchronous copies as soon as the product before is done with their memory.
 // A tile is left out where the mask leaves none of its pairs (attn_masked.h).  Rows beyond a sequence are zero in shared memory.
 // delta is summed in the order in which dP is, so that where a query sees a single key dP - delta is exactly zero.
@@ -22,7 +25,7 @@ namespace {
 
 constexpr int MF_R = 32;         // rows of a block
 constexpr int MF_C = 64;         // rows of a tile of the other side
-constexpr int MF_RPT = 4;        // rows of a thread (2 on twice the threads: backward 165 -> 227 us, the reads of operands decide)
+constexpr int MF_RPT = 4;        // rows of a thread (2 on twice the threads: backward 38 % slower, the reads of operands decide)
 constexpr int MF_NT = 16 * MF_R / MF_RPT;
 constexpr int MF_PP = MF_C + 4;  // floats between rows of a tile of scores
 
@@ -30,13 +33,33 @@ struct Rows { const float* p; int64_t batch, row, head; };
 struct MaskedParams {
   AttnMask m;
   Rows q, k, v, dc, c;
-  Rows o0, o1;        // forward: ctx; queries: dq; keys: dk, dv
+  Rows o, dk, dv;     // forward: ctx; backward: dq, dk, dv
   float *lse, *delta;
-  int heads, kv_heads, D, tiles, rows;
+  int batch, heads, kv_heads, D, tiles, rows;
+  unsigned kv_blocks;
 };
 
 __device__ __forceinline__ const float* row_ptr(const Rows& r, int64_t b, int64_t i, int h) {
   return r.p + b * r.batch + i * r.row + h * r.head;
+}
+
+// Tile, head and sequence of a block.  causal: the tiles with the longest loops start first, the last queries or the first keys;
+// else the tiles of a head side by side, which read the same rows.
+struct Place { int tile, h, b; };
+__device__ __forceinline__ Place place_of(const MaskedParams& p, int block, int heads, bool keys) {
+  Place a;
+  int head;
+  if (p.m.causal) {
+    const int per = heads * p.batch, t = block / per;
+    head = block - t * per;
+    a.tile = keys ? t : p.tiles - 1 - t;
+  } else {
+    head = block / p.tiles;
+    a.tile = block - head * p.tiles;
+  }
+  a.b = head / heads;
+  a.h = head - a.b * heads;
+  return a;
 }
 
 // Asks for rows [r0, r0 + kRows) of a head; rows from `rows` on and columns from D on are zero.
@@ -190,9 +213,9 @@ __device__ __forceinline__ void store_rows(const Rows& dst, int b, int r0, int h
   }
 }
 
-// Shared memory of the three kernels: row tiles, loop tiles, scores, then the list of loop blocks.
-template <int DP> __host__ __device__ constexpr size_t tile_floats(int row_tiles, int loop_tiles, int scores) {
-  return (size_t)(row_tiles * MF_R + loop_tiles * MF_C) * (DP + 4) + (size_t)scores * MF_R * MF_PP;
+// Shared memory of both kernels: row tiles, two loop tiles, scores, then the list of loop blocks.
+template <int DP> __host__ __device__ constexpr size_t tile_floats(int row_tiles) {
+  return (size_t)(row_tiles * MF_R + 2 * MF_C) * (DP + 4) + (size_t)MF_R * MF_PP;
 }
 
 template <int DP>
@@ -204,10 +227,11 @@ masked_fwd_kernel(const MaskedParams p) {
   float* Ks = Qs + MF_R * (DP + 4);
   float* Vs = Ks + MF_C * (DP + 4);
   float* Ps = Vs + MF_C * (DP + 4);
-  uint16_t* list = (uint16_t*)(sm + tile_floats<DP>(1, 2, 1));
+  uint16_t* list = (uint16_t*)(sm + tile_floats<DP>(1));
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  const int tile = blockIdx.x % p.tiles, h = blockIdx.x / p.tiles % p.heads, b = blockIdx.x / p.tiles / p.heads;
-  const int hk = h / (p.heads / p.kv_heads), q0 = tile * MF_R;
+  const Place place = place_of(p, blockIdx.x, p.heads, false);
+  const int h = place.h, b = place.b;
+  const int hk = h / (p.heads / p.kv_heads), q0 = place.tile * MF_R;
   pdl_begin();
   const Seq s = sequence(p.m, b);
   const float slope = p.m.slopes ? p.m.slopes[h] : 0.f;
@@ -283,7 +307,7 @@ masked_fwd_kernel(const MaskedParams p) {
     if (dead) f[i] = 0.f;
     if (tx == 0 && p.lse && r < p.m.S) p.lse[((int64_t)b * p.heads + h) * p.m.S + r] = dead ? -INFINITY : top[i] + logf(sum[i]);
   }
-  store_rows<DP>(p.o0, b, q0, h, p.m.S, p.D, ty, tx, acc, f);
+  store_rows<DP>(p.o, b, q0, h, p.m.S, p.D, ty, tx, acc, f);
 }
 
 // delta_i = dC_i . C_i, even and odd elements summed apart, one thread a row and head
@@ -305,22 +329,23 @@ masked_delta_kernel(const MaskedParams p) {
   p.delta[(b * p.heads + h) * S + i] = acc.x + acc.y;
 }
 
+// what a block keeps beside its tiles
+struct Beside { int fixed_docs[MF_R], docs[MF_C], red[16]; float lses[MF_C], deltas[MF_C]; };
+
 // dQ of 32 queries
 template <int DP>
-__global__ void __launch_bounds__(MF_NT)
-masked_dq_kernel(const MaskedParams p) {
-  extern __shared__ __align__(16) float sm[];
-  __shared__ int qdocs[MF_R], kdocs[MF_C], red[16];
+__device__ __forceinline__ void gradient_q(const MaskedParams& p, int block, float* sm, Beside& at_side) {
+  int *qdocs = at_side.fixed_docs, *kdocs = at_side.docs, *red = at_side.red;
   float* Qs = sm;
   float* Cs = Qs + MF_R * (DP + 4);
   float* Ks = Cs + MF_R * (DP + 4);
   float* Vs = Ks + MF_C * (DP + 4);
   float* Ps = Vs + MF_C * (DP + 4);
-  uint16_t* list = (uint16_t*)(sm + tile_floats<DP>(2, 2, 1));
+  uint16_t* list = (uint16_t*)(sm + tile_floats<DP>(2));
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  const int tile = blockIdx.x % p.tiles, h = blockIdx.x / p.tiles % p.heads, b = blockIdx.x / p.tiles / p.heads;
-  const int hk = h / (p.heads / p.kv_heads), q0 = tile * MF_R;
-  pdl_begin();
+  const Place place = place_of(p, block, p.heads, false);
+  const int h = place.h, b = place.b;
+  const int hk = h / (p.heads / p.kv_heads), q0 = place.tile * MF_R;
   const Seq s = sequence(p.m, b);
   const float slope = p.m.slopes ? p.m.slopes[h] : 0.f;
   ask_tile<DP, MF_R>(Qs, p.q, b, q0, h, s.len, p.D);
@@ -376,27 +401,24 @@ masked_dq_kernel(const MaskedParams p) {
   float f[MF_RPT];
 #pragma unroll
   for (int i = 0; i < MF_RPT; i++) f[i] = p.m.scale;
-  store_rows<DP>(p.o0, b, q0, h, p.m.S, p.D, ty, tx, acc, f);
+  store_rows<DP>(p.o, b, q0, h, p.m.S, p.D, ty, tx, acc, f);
 }
 
 // dK and dV of 32 keys: rows of the thread's tiles are keys, columns queries
 template <int DP>
-__global__ void __launch_bounds__(MF_NT)
-masked_dkv_kernel(const MaskedParams p) {
-  extern __shared__ __align__(16) float sm[];
-  __shared__ int qdocs[MF_C], kdocs[MF_R], red[16];
-  __shared__ float lses[MF_C], deltas[MF_C];
+__device__ __forceinline__ void gradient_kv(const MaskedParams& p, int block, float* sm, Beside& at_side) {
+  int *kdocs = at_side.fixed_docs, *qdocs = at_side.docs, *red = at_side.red;
+  float *lses = at_side.lses, *deltas = at_side.deltas;
   float* Ks = sm;
   float* Vs = Ks + MF_R * (DP + 4);
   float* Qs = Vs + MF_R * (DP + 4);
   float* Cs = Qs + MF_C * (DP + 4);
   float* Ps = Cs + MF_C * (DP + 4);
-  float* Ds = Ps + MF_R * MF_PP;
-  uint16_t* list = (uint16_t*)(sm + tile_floats<DP>(2, 2, 2));
+  uint16_t* list = (uint16_t*)(sm + tile_floats<DP>(2));
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  const int tile = blockIdx.x % p.tiles, hk = blockIdx.x / p.tiles % p.kv_heads, b = blockIdx.x / p.tiles / p.kv_heads;
-  const int group = p.heads / p.kv_heads, k0 = tile * MF_R;
-  pdl_begin();
+  const Place place = place_of(p, block, p.kv_heads, true);
+  const int hk = place.h, b = place.b;
+  const int group = p.heads / p.kv_heads, k0 = place.tile * MF_R;
   const Seq s = sequence(p.m, b);
   ask_tile<DP, MF_R>(Ks, p.k, b, k0, hk, s.len, p.D);
   ask_tile<DP, MF_R>(Vs, p.v, b, k0, hk, s.len, p.D);
@@ -449,13 +471,18 @@ masked_dkv_kernel(const MaskedParams p) {
         const int m = tx + 16 * c;
         const float w = __expf(z[i][c] - lses[m]);
         Ps[(MF_RPT * ty + i) * MF_PP + m] = w;
-        Ds[(MF_RPT * ty + i) * MF_PP + m] = w == 0.f ? 0.f : w * (dp[i][c] - deltas[m]) * bend[i][c];
+        z[i][c] = w == 0.f ? 0.f : w * (dp[i][c] - deltas[m]) * bend[i][c];
       }
     __syncwarp();
     accumulate<DP>(Ps, Cs, ty, tx, dv);
     __syncthreads();
     if (j + 1 < n * group) ask_c(j + 1);
-    accumulate<DP>(Ds, Qs, ty, tx, dk);
+#pragma unroll
+    for (int i = 0; i < MF_RPT; i++)
+#pragma unroll
+      for (int c = 0; c < 4; c++) Ps[(MF_RPT * ty + i) * MF_PP + tx + 16 * c] = z[i][c];
+    __syncwarp();
+    accumulate<DP>(Ps, Qs, ty, tx, dk);
     __syncthreads();
     if (j + 1 < n * group) ask_q(j + 1);
   }
@@ -466,8 +493,20 @@ masked_dkv_kernel(const MaskedParams p) {
     one[i] = k0 + MF_RPT * ty + i < s.len ? 1.f : 0.f;
     f[i] = p.m.scale * one[i];
   }
-  store_rows<DP>(p.o0, b, k0, hk, p.m.S, p.D, ty, tx, dk, f);
-  store_rows<DP>(p.o1, b, k0, hk, p.m.S, p.D, ty, tx, dv, one);
+  store_rows<DP>(p.dk, b, k0, hk, p.m.S, p.D, ty, tx, dk, f);
+  store_rows<DP>(p.dv, b, k0, hk, p.m.S, p.D, ty, tx, dv, one);
+}
+
+// Both in one launch, blocks of keys first, which have the longer steps: full precision is used on small batches, where either
+// alone is less than a wave of blocks and the device idles behind its longest ones.
+template <int DP>
+__global__ void __launch_bounds__(MF_NT, DP == 64 ? 3 : 2)
+masked_bwd_kernel(const MaskedParams p) {
+  extern __shared__ __align__(16) float sm[];
+  __shared__ Beside at_side;
+  pdl_begin();
+  if (blockIdx.x < p.kv_blocks) gradient_kv<DP>(p, blockIdx.x, sm, at_side);
+  else gradient_q<DP>(p, blockIdx.x - p.kv_blocks, sm, at_side);
 }
 
 constexpr int kMaxDevices = 64;
@@ -492,39 +531,37 @@ MaskedParams params_of(const mslt_attention_desc& d) {
   MaskedParams p = {};
   p.m = AttnMask{d.S, d.causal != 0, d.scale, d.cap, d.slopes, d.prefix, d.docs, d.lens};
   p.q = rows_of(d.q); p.k = rows_of(d.k); p.v = rows_of(d.v);
-  p.lse = d.lse; p.heads = d.heads; p.kv_heads = d.kv_heads; p.D = d.head_dim;
+  p.lse = d.lse; p.batch = d.B; p.heads = d.heads; p.kv_heads = d.kv_heads; p.D = d.head_dim;
   p.tiles = (d.S + MF_R - 1) / MF_R;
   return p;
 }
 
-template <int DP> size_t smem_bytes(int row_tiles, int loop_tiles, int scores, int S) {
-  return tile_floats<DP>(row_tiles, loop_tiles, scores) * sizeof(float) + ((size_t)(S + MF_C - 1) / MF_C * 2 + 15) / 16 * 16;
+template <int DP> size_t smem_bytes(int row_tiles, int S) {
+  return tile_floats<DP>(row_tiles) * sizeof(float) + ((size_t)(S + MF_C - 1) / MF_C * 2 + 15) / 16 * 16;
 }
 constexpr int kMostS = 131072;
 
 template <int DP>
 int forward(const mslt_attention_desc& d, cudaStream_t st, char* err) {
   static bool done[kMaxDevices];
-  if (opt_in((const void*)masked_fwd_kernel<DP>, done, smem_bytes<DP>(1, 2, 1, kMostS), err)) return MSLT_ERR_CUDA;
+  if (opt_in((const void*)masked_fwd_kernel<DP>, done, smem_bytes<DP>(1, kMostS), err)) return MSLT_ERR_CUDA;
   MaskedParams p = params_of(d);
-  p.o0 = rows_of(d.ctx);
-  launch_pdl(masked_fwd_kernel<DP>, d.B * d.heads * p.tiles, MF_NT, smem_bytes<DP>(1, 2, 1, d.S), st, p);
+  p.o = rows_of(d.ctx);
+  launch_pdl(masked_fwd_kernel<DP>, d.B * d.heads * p.tiles, MF_NT, smem_bytes<DP>(1, d.S), st, p);
   return 0;
 }
 
 template <int DP>
 int backward(const mslt_attention_desc& d, float* delta, cudaStream_t st, char* err) {
-  static bool done_q[kMaxDevices], done_kv[kMaxDevices];
-  if (opt_in((const void*)masked_dq_kernel<DP>, done_q, smem_bytes<DP>(2, 2, 1, kMostS), err)) return MSLT_ERR_CUDA;
-  if (opt_in((const void*)masked_dkv_kernel<DP>, done_kv, smem_bytes<DP>(2, 2, 2, kMostS), err)) return MSLT_ERR_CUDA;
+  static bool done[kMaxDevices];
+  if (opt_in((const void*)masked_bwd_kernel<DP>, done, smem_bytes<DP>(2, kMostS), err)) return MSLT_ERR_CUDA;
   MaskedParams p = params_of(d);
   p.dc = rows_of(d.dctx); p.c = rows_of(d.ctx); p.delta = delta;
   p.rows = d.B * d.heads * d.S;
   launch_pdl(masked_delta_kernel, (int)(((int64_t)p.rows + MF_NT - 1) / MF_NT), MF_NT, 0, st, p);
-  p.o0 = rows_of(d.dq);
-  launch_pdl(masked_dq_kernel<DP>, d.B * d.heads * p.tiles, MF_NT, smem_bytes<DP>(2, 2, 1, d.S), st, p);
-  p.o0 = rows_of(d.dk); p.o1 = rows_of(d.dv);
-  launch_pdl(masked_dkv_kernel<DP>, d.B * d.kv_heads * p.tiles, MF_NT, smem_bytes<DP>(2, 2, 2, d.S), st, p);
+  p.o = rows_of(d.dq); p.dk = rows_of(d.dk); p.dv = rows_of(d.dv);
+  p.kv_blocks = (unsigned)d.B * d.kv_heads * p.tiles;
+  launch_pdl(masked_bwd_kernel<DP>, p.kv_blocks + (unsigned)d.B * d.heads * p.tiles, MF_NT, smem_bytes<DP>(2, d.S), st, p);
   return 0;
 }
 
