@@ -14,9 +14,10 @@
 // tensor memory of 100, dependent instructions of three or four warps a scheduler.  So many warps share an SM: heads of 64, four
 // forward blocks (128 columns of tensor memory and 80 registers each), sixteen softmax warps of one backward block.
 // Measured with 37 tiles a head x 16 heads, all SMs full, cycles of an SM for 128 x 128 scores: forward 1690 (exponential unit
-// 59 % busy), dQ 2150 (52 %), dK and dV 2700 (42 %).  Tried on it: two forward blocks of double-buffered scores 2240; scores
-// held in registers by three blocks 2330; a quarter to a half of the backward's exponentials by polynomial 3 to 12 % slower;
-// eight backward softmax warps of 64 columns 3 % slower; polls with a suspend time: level.
+// 59 % busy; without `rest`, which takes 15 % more), dQ 2150 (52 %), dK and dV 2700 (42 %).  Tried on it: two forward blocks of
+// double-buffered scores 2240; scores held in registers by three blocks 2330; a quarter to a half of the backward's
+// exponentials by polynomial 3 to 12 % slower; eight backward softmax warps of 64 columns 3 % slower; polls with a suspend
+// time: level.
 //
 // Which blocks a row tile visits is worked out once, at its start, from positions, length, prefix and the least and
 // greatest document of either side: left out, whole, or with pairs to test.  Documents may be in any order; where they

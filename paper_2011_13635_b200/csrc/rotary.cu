@@ -9,7 +9,7 @@
 // apart, or side by side where neighbours are paired (and the rest of the head likewise).  So nothing is exchanged but
 // the norm's sums, and the lane's pairs are W neighbours of the table in either layout.  W is 4 in either type: 8 bf16 a
 // piece measure the same for the rotation alone (19.0 against 19.1 us at 16384 rows x 24 heads x 64) and leave the norm's
-// backward too few registers (77 against 55 us).  The angle of a pair depends on row and pair only: a warp works three
+// backward too few registers (77 against 55 us at the time).  The angle of a pair depends on row and pair only: a warp works three
 // groups of heads of a row with one set of cosines and sines, asks for all of their bytes before it forms them, and takes
 // the three sums of a norm side by side.  (One 16-byte piece a lane and the partner's values through shuffles: twice the
 // sines, 32 us.)  Angles: the table holds turns a position as 64-bit fractions, position times table modulo 2^64 is the turn's
@@ -39,32 +39,35 @@ struct RotaryParams {
   float magnitude, sign, eps;
 };
 
-constexpr int W = 4;  // elements of a piece
+constexpr int W = 4;  // elements of a piece, in pairs for packed arithmetic
 
 template <typename T> struct Piece;
 template <> struct Piece<float> {
   typedef float4 Raw;
-  static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[W]) { VecT<float>::unpack(r, v); }
-  static __device__ __forceinline__ void store(float* p, const float (&v)[W]) { VecT<float>::store(p, v); }
+  static __device__ __forceinline__ void unpack(const Raw& r, float2 (&v)[2]) {
+    v[0] = make_float2(r.x, r.y);
+    v[1] = make_float2(r.z, r.w);
+  }
+  static __device__ __forceinline__ void store(float* p, const float2 (&v)[2]) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+  }
 };
 template <> struct Piece<bf16> {
   typedef uint2 Raw;
-  static __device__ __forceinline__ void unpack(const Raw& r, float (&v)[W]) {
-    const uint32_t w[2] = {r.x, r.y};
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+  static __device__ __forceinline__ void unpack(const Raw& r, float2 (&v)[2]) {
+    v[0] = make_float2(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u));
+    v[1] = make_float2(__uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
   }
-  static __device__ __forceinline__ void store(bf16* p, const float (&v)[W]) {
+  static __device__ __forceinline__ void store(bf16* p, const float2 (&v)[2]) {
     uint2 r;
     __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&r);
-    h[0] = __floats2bfloat162_rn(v[0], v[1]);
-    h[1] = __floats2bfloat162_rn(v[2], v[3]);
+    h[0] = __floats2bfloat162_rn(v[0].x, v[0].y);
+    h[1] = __floats2bfloat162_rn(v[1].x, v[1].y);
     *reinterpret_cast<uint2*>(p) = r;
   }
 };
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 pair_at(const float* p) { return *reinterpret_cast<const float2*>(p); }
 
 __device__ __forceinline__ void turn_of(int pos, uint64_t turns, bool exact, float& s, float& c) {
   const int32_t f = (int32_t)(((uint64_t)(int64_t)pos * turns) >> 32);
@@ -89,29 +92,32 @@ __device__ __forceinline__ void lanes_sum(float (&v)[N], int lanes) {
     }
 }
 
-// The lane's pairs turned: (a_j, b_j), or the neighbours in a and in b.  What does not turn is left as it is.
-template <bool INTER>
-__device__ __forceinline__ void rotate(float (&a)[W], float (&b)[W], const float (&c)[W], const float (&s)[W], bool turn_a, bool turn_b) {
+// The lane's pairs turned: (a_j, b_j), or the neighbours in a and in b; c, s, minus s by pair.  What does not turn is left as it is.
+// kPacked: two pairs an instruction, where the norms' instructions count; the rotation alone has no registers for minus s.
+template <bool INTER, bool kPacked>
+__device__ __forceinline__ void rotate(float2 (&a)[2], float2 (&b)[2], const float2 (&c)[2], const float2 (&s)[2], const float2 (&ms)[2],
+                                       bool turn_a, bool turn_b) {
   if (INTER) {
-#pragma unroll
-    for (int j = 0; j < W / 2; j++) {
-      if (turn_a) {
-        const float u = a[2 * j], w = a[2 * j + 1];
-        a[2 * j] = fmaf(-w, s[j], u * c[j]);
-        a[2 * j + 1] = fmaf(u, s[j], w * c[j]);
-      }
-      if (turn_b) {
-        const float u = b[2 * j], w = b[2 * j + 1], cb = c[W / 2 + j], sb = s[W / 2 + j];
-        b[2 * j] = fmaf(-w, sb, u * cb);
-        b[2 * j + 1] = fmaf(u, sb, w * cb);
-      }
+    auto turn = [](float2& v, float cs, float sn) { v = make_float2(fmaf(-v.y, sn, v.x * cs), fmaf(v.x, sn, v.y * cs)); };
+    if (turn_a) {
+      turn(a[0], c[0].x, s[0].x);
+      turn(a[1], c[0].y, s[0].y);
+    }
+    if (turn_b) {
+      turn(b[0], c[1].x, s[1].x);
+      turn(b[1], c[1].y, s[1].y);
     }
   } else if (turn_a) {
 #pragma unroll
-    for (int j = 0; j < W; j++) {
-      const float u = a[j], w = b[j];
-      a[j] = fmaf(-w, s[j], u * c[j]);
-      b[j] = fmaf(u, s[j], w * c[j]);
+    for (int j = 0; j < 2; j++) {
+      const float2 u = a[j], w = b[j];
+      if (kPacked) {
+        a[j] = __ffma2_rn(w, ms[j], __fmul2_rn(u, c[j]));
+        b[j] = __ffma2_rn(u, s[j], __fmul2_rn(w, c[j]));
+      } else {
+        a[j] = make_float2(fmaf(-w.x, s[j].x, u.x * c[j].x), fmaf(-w.y, s[j].y, u.y * c[j].y));
+        b[j] = make_float2(fmaf(u.x, s[j].x, w.x * c[j].x), fmaf(u.y, s[j].y, w.y * c[j].y));
+      }
     }
   }
 }
@@ -119,9 +125,9 @@ __device__ __forceinline__ void rotate(float (&a)[W], float (&b)[W], const float
 // OP 0: rotation, 1: norm and rotation, 2: backward of 1.  A warp takes the heads of a row in passes of `together`; in the
 // backward queries and keys are taken by different blocks (grid y), each with one set of sums in registers.
 // PASSES, and BLOCKS of 256 threads on an SM (80 or 128 registers), were tried together; 16384 rows x 24 heads x 64 and 8144 x 20
-// x 128, us: rotation 3 x 4 18.8 and 16.2, 3 x 3 19.7 and 18.5, 2 x 3 21.6 and 18.5; norm 2 x 3 25.6 and 23.9, 3 x 3 32 and
-// 27, 3 x 2 27 and 28; backward 3 x 2 44 and 43, 2 x 3 54 and 40.  Rotation in fp32, 8168 x 32 x 64:
-// 4 x 2 24.5, 2 x 3 24.9, 4 x 3 28.4, 3 x 4 31.1.  Asking for a row ahead gained nothing at any of them.
+// x 128, us: rotation 3 x 4 18.9 and 16.0, 3 x 3 19.7 and 18.5, 2 x 3 20.3 and 16.1; norm 2 x 3 24.9 and 21.5, 3 x 3 29 and
+// 22.5, 2 x 4 27 and 19.8; backward 3 x 2 40.0 and 39.4 (43.6 and 42.1 without packed arithmetic), 2 x 3 63 and 43.  Rotation in
+// fp32, 8168 x 32 x 64: 4 x 2 24.5, 2 x 3 24.9, 4 x 3 28.4, 3 x 4 31.1.  Asking for a row ahead gained nothing at any of them.
 template <typename T, int OP> struct Shape {
   static constexpr bool wide = sizeof(T) == 4 && OP == 0;
   static constexpr int PASSES = wide ? 4 : OP == 1 ? 2 : 3, BLOCKS = wide ? 2 : OP == 0 ? 4 : OP == 1 ? 3 : 2;
@@ -157,9 +163,9 @@ rotary_kernel(const RotaryParams p) {
     }
   }
   __syncthreads();
-  float dga[W], dgb[W], dba[W], dbb[W];
+  float2 dga[2], dgb[2], dba[2], dbb[2];
 #pragma unroll
-  for (int j = 0; j < W; j++) dga[j] = dgb[j] = dba[j] = dbb[j] = 0.f;
+  for (int j = 0; j < 2; j++) dga[j] = dgb[j] = dba[j] = dbb[j] = make_float2(0.f, 0.f);
 
   const T* x0 = (const T*)p.x + h0 * p.x_head;
   const T* d0 = (const T*)p.dy + h0 * p.dy_head;
@@ -187,12 +193,14 @@ rotary_kernel(const RotaryParams p) {
         }
       }
     }
-    float c[W], s[W];
+    float2 c[2], s[2], ms[2];
 #pragma unroll
-    for (int j = 0; j < W; j++) {
-      turn_of(pos, turns[(o + j) & 63], kExact, s[j], c[j]);
-      s[j] *= p.sign * p.magnitude;
-      c[j] *= p.magnitude;
+    for (int j = 0; j < 2; j++) {
+      turn_of(pos, turns[(o + 2 * j) & 63], kExact, s[j].x, c[j].x);
+      turn_of(pos, turns[(o + 2 * j + 1) & 63], kExact, s[j].y, c[j].y);
+      ms[j] = __fmul2_rn(s[j], both(-p.sign * p.magnitude));
+      s[j] = __fmul2_rn(s[j], both(p.sign * p.magnitude));
+      c[j] = __fmul2_rn(c[j], both(p.magnitude));
     }
     float mean[PASSES], r[PASSES];
     if (OP >= 1) {
@@ -201,11 +209,11 @@ rotary_kernel(const RotaryParams p) {
       if (p.center) {
 #pragma unroll
         for (int k = 0; k < PASSES; k++) {
-          float a[W], b[W];
+          float2 a[2], b[2];
           Pc::unpack(xa[k], a);
           Pc::unpack(xb[k], b);
-#pragma unroll
-          for (int j = 0; j < W; j++) mean[k] += a[j] + b[j];
+          const float2 t = __fadd2_rn(__fadd2_rn(a[0], a[1]), __fadd2_rn(b[0], b[1]));
+          mean[k] = t.x + t.y;
         }
         lanes_sum(mean, lanes);
 #pragma unroll
@@ -213,28 +221,29 @@ rotary_kernel(const RotaryParams p) {
       }
 #pragma unroll
       for (int k = 0; k < PASSES; k++) {
-        float a[W], b[W];
+        float2 a[2], b[2], t = make_float2(0.f, 0.f);
         Pc::unpack(xa[k], a);
         Pc::unpack(xb[k], b);
 #pragma unroll
-        for (int j = 0; j < W; j++) {
-          a[j] -= mean[k];
-          b[j] -= mean[k];
-          r[k] = fmaf(a[j], a[j], r[k]);
-          r[k] = fmaf(b[j], b[j], r[k]);
+        for (int j = 0; j < 2; j++) {
+          a[j] = __fadd2_rn(a[j], both(-mean[k]));
+          b[j] = __fadd2_rn(b[j], both(-mean[k]));
+          t = __ffma2_rn(a[j], a[j], t);
+          t = __ffma2_rn(b[j], b[j], t);
         }
+        r[k] = t.x + t.y;
       }
       lanes_sum(r, lanes);
 #pragma unroll
       for (int k = 0; k < PASSES; k++) r[k] = rsqrtf(fmaf(r[k], inv_d, p.eps));
     }
     if (OP == 2) {
-      float a[PASSES][W], b[PASSES][W], u[PASSES][W], w[PASSES][W], m1[PASSES], m2[PASSES];
-      float ga[W], gb[W];
+      float2 a[PASSES][2], b[PASSES][2], u[PASSES][2], w[PASSES][2], ga[2], gb[2];
+      float m1[PASSES], m2[PASSES];
 #pragma unroll
-      for (int j = 0; j < W; j++) {
-        ga[j] = live ? gains[kind][ea + j] : 0.f;
-        gb[j] = live ? gains[kind][eb + j] : 0.f;
+      for (int j = 0; j < 2; j++) {
+        ga[j] = live ? pair_at(&gains[kind][ea + 2 * j]) : make_float2(0.f, 0.f);
+        gb[j] = live ? pair_at(&gains[kind][eb + 2 * j]) : make_float2(0.f, 0.f);
       }
 #pragma unroll
       for (int k = 0; k < PASSES; k++) {
@@ -242,33 +251,35 @@ rotary_kernel(const RotaryParams p) {
         Pc::unpack(xb[k], b[k]);
         Pc::unpack(da[k], u[k]);
         Pc::unpack(db[k], w[k]);
-        rotate<INTER>(u[k], w[k], c, s, turn_a, turn_b);
-        m1[k] = m2[k] = 0.f;
+        rotate<INTER, (OP >= 1)>(u[k], w[k], c, s, ms, turn_a, turn_b);
+        float2 t1 = make_float2(0.f, 0.f), t2 = t1;
 #pragma unroll
-        for (int j = 0; j < W; j++) {
-          a[k][j] = (a[k][j] - mean[k]) * r[k];  // xh
-          b[k][j] = (b[k][j] - mean[k]) * r[k];
-          dga[j] = fmaf(u[k][j], a[k][j], dga[j]);
-          dgb[j] = fmaf(w[k][j], b[k][j], dgb[j]);
-          dba[j] += u[k][j];
-          dbb[j] += w[k][j];
-          u[k][j] *= ga[j];
-          w[k][j] *= gb[j];
-          m1[k] = fmaf(u[k][j], a[k][j], m1[k]);
-          m1[k] = fmaf(w[k][j], b[k][j], m1[k]);
-          m2[k] += u[k][j] + w[k][j];
+        for (int j = 0; j < 2; j++) {
+          a[k][j] = __fmul2_rn(__fadd2_rn(a[k][j], both(-mean[k])), both(r[k]));  // xh
+          b[k][j] = __fmul2_rn(__fadd2_rn(b[k][j], both(-mean[k])), both(r[k]));
+          dga[j] = __ffma2_rn(u[k][j], a[k][j], dga[j]);
+          dgb[j] = __ffma2_rn(w[k][j], b[k][j], dgb[j]);
+          dba[j] = __fadd2_rn(dba[j], u[k][j]);
+          dbb[j] = __fadd2_rn(dbb[j], w[k][j]);
+          u[k][j] = __fmul2_rn(u[k][j], ga[j]);
+          w[k][j] = __fmul2_rn(w[k][j], gb[j]);
+          t1 = __ffma2_rn(u[k][j], a[k][j], t1);
+          t1 = __ffma2_rn(w[k][j], b[k][j], t1);
+          t2 = __fadd2_rn(t2, __fadd2_rn(u[k][j], w[k][j]));
         }
+        m1[k] = t1.x + t1.y;
+        m2[k] = t2.x + t2.y;
       }
       lanes_sum(m1, lanes);
       if (p.center) lanes_sum(m2, lanes);
 #pragma unroll
       for (int k = 0; k < PASSES; k++) {
-        m1[k] *= inv_d;
-        m2[k] = p.center ? m2[k] * inv_d : 0.f;
+        m1[k] *= -inv_d;
+        m2[k] = p.center ? m2[k] * -inv_d : 0.f;
 #pragma unroll
-        for (int j = 0; j < W; j++) {
-          a[k][j] = r[k] * (u[k][j] - m2[k] - a[k][j] * m1[k]);
-          b[k][j] = r[k] * (w[k][j] - m2[k] - b[k][j] * m1[k]);
+        for (int j = 0; j < 2; j++) {
+          a[k][j] = __fmul2_rn(both(r[k]), __ffma2_rn(a[k][j], both(m1[k]), __fadd2_rn(u[k][j], both(m2[k]))));
+          b[k][j] = __fmul2_rn(both(r[k]), __ffma2_rn(b[k][j], both(m1[k]), __fadd2_rn(w[k][j], both(m2[k]))));
         }
         if (here[k]) {
           T* out = out0 + row * out_row + k * out_step;
@@ -280,26 +291,26 @@ rotary_kernel(const RotaryParams p) {
 #pragma unroll
       for (int k = 0; k < PASSES; k++) {
         if (!here[k]) continue;
-        float a[W], b[W];
+        float2 a[2], b[2];
         Pc::unpack(xa[k], a);
         Pc::unpack(xb[k], b);
         if (OP == 1) {
           const int kd = h0 + k * together >= p.q_heads;
-          const float4 ga = *reinterpret_cast<const float4*>(&gains[kd][ea]), gb = *reinterpret_cast<const float4*>(&gains[kd][eb]);
-          float4 ba = make_float4(0.f, 0.f, 0.f, 0.f), bb = ba;
-          if (p.bias) {
-            ba = *reinterpret_cast<const float4*>(&biases[kd][ea]);
-            bb = *reinterpret_cast<const float4*>(&biases[kd][eb]);
-          }
-          const float g4[2][W] = {{ga.x, ga.y, ga.z, ga.w}, {gb.x, gb.y, gb.z, gb.w}};
-          const float b4[2][W] = {{ba.x, ba.y, ba.z, ba.w}, {bb.x, bb.y, bb.z, bb.w}};
 #pragma unroll
-          for (int j = 0; j < W; j++) {
-            a[j] = fmaf((a[j] - mean[k]) * r[k], g4[0][j], b4[0][j]);
-            b[j] = fmaf((b[j] - mean[k]) * r[k], g4[1][j], b4[1][j]);
+          for (int j = 0; j < 2; j++) {
+            a[j] = __fmul2_rn(__fadd2_rn(a[j], both(-mean[k])), both(r[k]));
+            b[j] = __fmul2_rn(__fadd2_rn(b[j], both(-mean[k])), both(r[k]));
+            const float2 ga = pair_at(&gains[kd][ea + 2 * j]), gb = pair_at(&gains[kd][eb + 2 * j]);
+            if (p.bias) {
+              a[j] = __ffma2_rn(a[j], ga, pair_at(&biases[kd][ea + 2 * j]));
+              b[j] = __ffma2_rn(b[j], gb, pair_at(&biases[kd][eb + 2 * j]));
+            } else {
+              a[j] = __fmul2_rn(a[j], ga);
+              b[j] = __fmul2_rn(b[j], gb);
+            }
           }
         }
-        rotate<INTER>(a, b, c, s, turn_a, turn_b);
+        rotate<INTER, (OP >= 1)>(a, b, c, s, ms, turn_a, turn_b);
         T* out = out0 + row * out_row + k * out_step;
         Pc::store(out + ea, a);
         Pc::store(out + eb, b);
@@ -308,14 +319,14 @@ rotary_kernel(const RotaryParams p) {
   }
 
   if (OP == 2) {  // the block's sums, warps and groups in order
-    __shared__ float part[RO_WARPS][2][64 * W];  // together * D <= 64 W
+    __shared__ __align__(16) float part[RO_WARPS][2][64 * W];  // together * D <= 64 W
     if (live) {
 #pragma unroll
-      for (int j = 0; j < W; j++) {
-        part[warp][0][sub * p.D + ea + j] = dga[j];
-        part[warp][0][sub * p.D + eb + j] = dgb[j];
-        part[warp][1][sub * p.D + ea + j] = dba[j];
-        part[warp][1][sub * p.D + eb + j] = dbb[j];
+      for (int j = 0; j < 2; j++) {
+        *reinterpret_cast<float2*>(&part[warp][0][sub * p.D + ea + 2 * j]) = dga[j];
+        *reinterpret_cast<float2*>(&part[warp][0][sub * p.D + eb + 2 * j]) = dgb[j];
+        *reinterpret_cast<float2*>(&part[warp][1][sub * p.D + ea + 2 * j]) = dba[j];
+        *reinterpret_cast<float2*>(&part[warp][1][sub * p.D + eb + 2 * j]) = dbb[j];
       }
     }
     __syncthreads();
