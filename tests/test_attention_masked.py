@@ -387,6 +387,66 @@ def test_every_block_of_a_large_launch_ends(dim, kw):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,causal", [("fp32", False), ("bf16", False), ("bf16", True)])
+def test_the_longest_row_with_offsets_beyond_32_bits(dtype, causal):
+    """131072 tokens, 16416 elements apart: documents in the middle, at the end, and one of the first and last tokens."""
+    import torch
+    from paper_2011_13635_b200 import binding as B
+    S, row, dim = 131072, 16416, 64
+    t = torch.float32 if dtype == "fp32" else torch.bfloat16
+    store = torch.empty(S, row, dtype=t, device="cuda")
+    at = lambda i: store[:, row - (i + 1) * dim:row - i * dim].view(1, S, 1, dim)                            # noqa: E731
+    names = ("q", "k", "v", "dc", "ctx", "low", "dq", "dk", "dv")
+    x = {n: at(i) for i, n in enumerate(names)}
+    assert (S - 1) * row > 1 << 31
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for n in names[:4]:
+        x[n].copy_(torch.randn(1, S, 1, dim, generator=g, device="cuda"))
+    docs = torch.arange(S, device="cuda", dtype=torch.int32) // 1000 + 10
+    docs[:100] = docs[-72:] = 7
+    low = x["low"] if dtype == "bf16" else None
+    lse, status = torch.empty(1, 1, S, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(B.mslt_op_attention_masked_bwd_scratch_bytes(1, S, 1), dtype=torch.uint8, device="cuda")
+    kw = dict(docs=docs[None], causal=causal, rest=low)
+    B.mslt_op_attention_masked(x["q"], x["k"], x["v"], x["ctx"], lse, 0.125, status, _stream(), **kw)
+    B.mslt_op_attention_masked_bwd(x["q"], x["k"], x["v"], x["ctx"], lse, x["dc"], x["dq"], x["dk"], x["dv"], scratch, 0.125, status,
+                                   _stream(), **kw)
+    for which in (75, 140, 7):
+        rows = (docs == which).nonzero()[:, 0]
+        part = {n: x[n][:, rows] for n in names}
+        part.update(scale=0.125, mask=dict(cap=0.0, causal=causal, prefix=None, docs=None, lens=None, slopes=None))
+        check(part, dict(ctx=part["ctx"], lse=lse[:, :, rows], dq=part["dq"], dk=part["dk"], dv=part["dv"]))
+
+
+@pytest.mark.gpu
+def test_the_longest_row_whole():
+    """Every key of 131072 seen by every query: context, lse and dq of a few queries."""
+    import torch
+    S, dim = 131072, 64
+    s = make("bf16", 1, S, 1, 1, dim)
+    out = run(s)
+    rows = [0, 1, 65535, 65536, S - 1]
+    D = lambda v: v[0, :, 0].double()                                                                       # noqa: E731
+    q, k, v, dc = D(s["q"])[rows], D(s["k"]), D(s["v"]), D(s["dc"])[rows]
+    z = q @ k.T * 0.125
+    p, lse = torch.softmax(z, -1), torch.logsumexp(z, -1)
+    u = 2.0 ** -8
+    # scores as in `check`; a row's sum has 2 x 65536 terms added one after the other
+    e_row = ((dim + 8) * F32 * (q.abs() @ k.abs().T) * 0.125 + 4 * F32 * z.abs()).amax(-1) + 2.0 ** -21 + S * F32
+    assert ((out["lse"][0, 0, rows] - lse).abs() <= e_row + 4 * F32 * (lse.abs() + z.amax(-1).abs())).all()
+    rel = (2 * u * u + 2 * e_row)[:, None]
+    o, big = p @ v, p @ v.abs()
+    assert ((D(out["ctx"])[rows] - o).abs() <= (rel + S * F32) * big + u * o.abs()).all()
+    dp = dc @ v.T
+    delta = (p * dp).sum(-1, keepdim=True)
+    ds = p * (dp - delta)
+    e_delta = ((rel + S * F32) * (dc.abs() * big).sum(-1, keepdim=True) + (2.0 ** -16 + (dim + 8) * F32) * (dc.abs() * o.abs()).sum(-1, keepdim=True))
+    e_ds = p * ((dp - delta).abs() * 2 * e_row[:, None] + (dim + 8) * F32 * (dc.abs() @ v.abs().T) + e_delta) + u * ds.abs()
+    dq = ds @ k * 0.125
+    assert ((D(out["dq"])[rows] - dq).abs() <= 0.125 * (1.01 * e_ds @ k.abs() + S * F32 * (ds.abs() @ k.abs())) + u * dq.abs()).all()
+
+
+@pytest.mark.gpu
 def test_a_wait_that_runs_out_is_reported():
     """The producer of the next launch issues no copies: status after 20 ms, and the device stays usable."""
     import torch
