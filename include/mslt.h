@@ -502,7 +502,7 @@ int mslt_rope_turns(int32_t rot_dim, double base, int32_t scaling, double factor
  * The backward call takes the forward's x again, forms the statistics from it, and writes dx, d_dgain and, where not
  * NULL, d_dbias (written, not added to; sums in a fixed order: the same bits on every run).  dx may be dy itself with the
  * same strides.  d_scratch: device, 16-byte aligned, of mslt_op_qk_norm_rope_bwd_scratch_bytes bytes; contents on entry
- * do not matter.
+ * do not matter; calls in flight at once need one each.
  */
 typedef struct {
   mslt_rope_desc rope;   /* x, y as in mslt_op_rope (the backward call does not use y); inverse must be 0; rot_dim may be 0 */
@@ -562,7 +562,7 @@ typedef struct {
 } mslt_attention_desc;
 /* d_status and sync as in mslt_op_attention. */
 int mslt_op_attention_masked(const mslt_attention_desc* desc, int32_t* d_status, void* cuda_stream, int32_t sync);
-/* d_scratch: device, 16-byte aligned; contents on entry do not matter. */
+/* d_scratch: device, 16-byte aligned; contents on entry do not matter; calls in flight at once need one each. */
 size_t mslt_op_attention_masked_bwd_scratch_bytes(int32_t B, int32_t S, int32_t heads);
 int mslt_op_attention_masked_bwd(const mslt_attention_desc* desc, void* d_scratch, size_t scratch_bytes, int32_t* d_status,
                                  void* cuda_stream, int32_t sync);

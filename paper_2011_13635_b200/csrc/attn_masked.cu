@@ -73,6 +73,9 @@ int end_attention(const char* what, const int32_t* status, cudaStream_t st, int 
   return 0;
 }
 
+// delta of the backward call; the counters of its bf16 kernels follow
+size_t delta_bytes(int32_t B, int32_t S, int32_t heads) { return ((size_t)B * S * heads * sizeof(float) + 255) / 256 * 256; }
+
 }  // namespace
 
 extern "C" {
@@ -94,7 +97,7 @@ int mslt_op_attention_masked(const mslt_attention_desc* caller, int32_t* d_statu
 
 size_t mslt_op_attention_masked_bwd_scratch_bytes(int32_t B, int32_t S, int32_t heads) {
   if (B < 1 || S < 1 || heads < 1) return 0;
-  return ((size_t)B * S * heads * sizeof(float) + 255) / 256 * 256;
+  return delta_bytes(B, S, heads) + 256;
 }
 
 int mslt_op_attention_masked_bwd(const mslt_attention_desc* caller, void* d_scratch, size_t scratch_bytes, int32_t* d_status,
@@ -116,7 +119,8 @@ int mslt_op_attention_masked_bwd(const mslt_attention_desc* caller, void* d_scra
   if ((rc = op_need_device())) return rc;
   return op_nothrow(what, [&] {
     char err[256] = "";
-    int r = desc->dtype == 1 ? attn_masked_tc_bwd(*desc, (float*)d_scratch, d_status, (cudaStream_t)cuda_stream, err)
+    int* next = (int*)((char*)d_scratch + delta_bytes(desc->B, desc->S, desc->heads));
+    int r = desc->dtype == 1 ? attn_masked_tc_bwd(*desc, (float*)d_scratch, next, d_status, (cudaStream_t)cuda_stream, err)
                              : attn_masked_f32_bwd(*desc, (float*)d_scratch, (cudaStream_t)cuda_stream, err);
     if (r) return op_refuse(r, "%s", err);
     return end_attention(what, d_status, (cudaStream_t)cuda_stream, sync);

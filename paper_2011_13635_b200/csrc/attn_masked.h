@@ -115,6 +115,6 @@ __device__ __forceinline__ int list_blocks(const AttnMask& m, const Seq& s, int 
 int attn_masked_f32_fwd(const mslt_attention_desc& d, cudaStream_t st, char* err);
 int attn_masked_f32_bwd(const mslt_attention_desc& d, float* delta, cudaStream_t st, char* err);
 int attn_masked_tc_fwd(const mslt_attention_desc& d, int* status, cudaStream_t st, char* err);
-int attn_masked_tc_bwd(const mslt_attention_desc& d, float* delta, int* status, cudaStream_t st, char* err);
+int attn_masked_tc_bwd(const mslt_attention_desc& d, float* delta, int* next, int* status, cudaStream_t st, char* err);
 
 }  // namespace mslt

@@ -62,6 +62,7 @@ struct TcParams {
   bf16* rest;
   float* lse;
   const float* delta;
+  int* next;            // backward: tiles taken so far beyond the first of every block; zero when the kernel starts
   int a_perm[3], b_perm[3], c_perm[3], d_perm[3];
   long long wait_limit;
   int starve;           // test hook: the producer issues no copies, so the first wait runs out
@@ -764,10 +765,11 @@ masked_fwd_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ C
 
 // ---- backward ---------------------------------------------------------------------------------------------
 
-// delta_i = dC_i . (C_i + rest_i): eight elements a lane, the lanes of a row side by side
+// delta_i = dC_i . (C_i + rest_i), and the counters of the kernels behind it: eight elements a lane, the lanes of a row side by side
 __global__ void __launch_bounds__(256)
-masked_delta_tc(const View dc, const View c, const bf16* rest, float* delta, int S, int heads, int D, int log_lanes, long long rows) {
+masked_delta_tc(const View dc, const View c, const bf16* rest, float* delta, int* next, int S, int heads, int D, int log_lanes, long long rows) {
   pdl_begin();
+  if (blockIdx.x == 0 && threadIdx.x < 2) next[threadIdx.x] = 0;
   const int lanes = 1 << log_lanes;
   const long long n = ((long long)blockIdx.x * 256 + threadIdx.x) >> log_lanes;  // head fastest: neighbours in memory
   const int e = (threadIdx.x & (lanes - 1)) * 8;
@@ -817,14 +819,14 @@ static_assert(BwdShape<64, true>::ACC_COL + 2 * 64 <= 512 && BwdShape<128, false
 
 // kKeys = false: rows are queries (A = q, B = k, C = dctx, D = v; loop over keys), the result is dq.
 // kKeys = true: rows are keys (A = k, B = q, C = v, D = dctx; loop over the queries of every head that shares them): dk, dv.
-// Persistent, a block an SM: row tiles in turn, steps counted on from tile to tile so that the barriers' phases go on.  The
+// Persistent, a block an SM: row tiles as they come (a counter: which block takes a tile changes no sum), steps counted on from tile to tile so that the barriers' phases go on.  The
 // producer warp works out a tile's list and asks for its rows while the tile before is under way; only the reading of
 // the accumulators lies between two tiles.  (A launch of a block a tile: 8 x 12 x 2048 in 6 documents 344 us.)
 template <int DP, bool kKeys, int kForm>
 __global__ void __launch_bounds__(AB_THREADS, 1)
 masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
               const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmD, const TcParams p) {
-  enum { I_LIST, I_LEN, I_PREFIX, I_ROW, I_HEAD, I_BATCH };  // entries of its list, length, prefix, first row, head, sequence
+  enum { I_LIST, I_LEN, I_PREFIX, I_ROW, I_HEAD, I_BATCH };  // entries of its list (-1: no tile), length, prefix, first row, head, sequence
   typedef BwdShape<DP, kKeys> Sh;
   constexpr int NS = Sh::STAGES, FB = Sh::FB, SB = Sh::SB, PB = Sh::PB, LOOP = Sh::LOOP, PART = Sh::PART;
   extern __shared__ uint8_t smem_raw[];
@@ -896,12 +898,21 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     // ------------------------------- producer -------------------------------
     int g = 0, tiles_done = 0, i = 0;  // steps and tiles so far
     bool ok = true;
-    for (int w = blockIdx.x; w < items; w += gridDim.x, i++) {
-      const Item it = item_at(w);
+    int taken = 0;
+    for (int w = blockIdx.x;; w = (int)gridDim.x + __shfl_sync(0xffffffffu, taken, 0), i++) {
+      const Item it = item_at(min(w, items - 1));
       const int slot = i & 1;
+      if (lane == 0 && w < items) taken = atomicAdd(p.next, 1);  // asked for a tile ahead
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&listempty[slot]), (uint32_t)(i >> 1 & 1) ^ 1, abort_flag, p.status));
       int n_list = 0;
       uint16_t* list = lists + slot * p.list_room;
+      if (ok && w >= items) {
+        if (lane == 0) {
+          info[slot][I_LIST] = -1;  // no more tiles
+          mbar_arrive(smem_u32(&listfull[slot]));
+        }
+        break;
+      }
       if (ok) {
         const Seq s = sequence(p.m, it.b);
         n_list = list_blocks_warp<kKeys, LOOP>(p.m, s, it.b, it.r0, list);
@@ -963,10 +974,11 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     auto landed = [&](int j) { return mbar_wait(smem_u32(&full[j % NS]), j / NS & 1, abort_flag, p.status); };
     int g = 0, tiles_done = 0, i = 0;
     bool ok = true;
-    for (int w = blockIdx.x; w < items && ok; w += gridDim.x, i++) {
+    for (; ok; i++) {
       const int slot = i & 1;
       if (!mbar_wait(smem_u32(&listfull[slot]), i >> 1 & 1, abort_flag, p.status)) { ok = false; break; }
       const int n = info[slot][I_LIST] * spans;
+      if (n < 0) break;
       mbar_arrive(smem_u32(&listempty[slot]));
       if (n == 0) continue;
       const int f = tiles_done % FB;
@@ -1043,14 +1055,15 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     auto enter = [&](int tile) {  // the block's tile-th tile
       if (!mbar_wait(smem_u32(&listfull[tile & 1]), tile >> 1 & 1, abort_flag, p.status)) return false;
       it = info[tile & 1];
+      if (it[I_LIST] < 0) return true;
       const int r = it[I_ROW] + quarter * 32 + lane;
       if (!kKeys) ask(it[I_HEAD], r);
       if (p.m.docs) doc = r < it[I_LEN] ? p.m.docs[(long long)it[I_BATCH] * p.m.S + r] : 0;
       if (it[I_LIST] > 0) ask_step(kKeys ? it[I_HEAD] * group : 0, lists[(tile & 1) * p.list_room]);
       return true;
     };
-    if ((int)blockIdx.x < items) ok = enter(0);
-    for (int w = blockIdx.x; w < items && ok; w += gridDim.x, i++) {
+    ok = enter(0);
+    for (; ok && it[I_LIST] >= 0; i++) {
       const int slot = i & 1;
       const int n_list = it[I_LIST], n = n_list * spans, r = it[I_ROW] + quarter * 32 + lane;
       const uint16_t* list = lists + slot * p.list_room;
@@ -1181,7 +1194,7 @@ masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       const bool dead = r >= it[I_LEN], write = r < p.m.S;
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&listempty[slot]));
-      if (w + (int)gridDim.x < items && !enter(i + 1)) { ok = false; break; }
+      if (!enter(i + 1)) { ok = false; break; }
       if (n > 0) {
         if (!mbar_wait(smem_u32(&done), tiles_done & 1, abort_flag, p.status)) { ok = false; break; }
         tc_fence_after();
@@ -1307,7 +1320,7 @@ int attn_masked_tc_fwd(const mslt_attention_desc& d, int* status, cudaStream_t s
   return form == 0 ? forward<128, 0>(d, p, m, st, err) : form == 1 ? forward<128, 1>(d, p, m, st, err) : forward<128, 2>(d, p, m, st, err);
 }
 
-int attn_masked_tc_bwd(const mslt_attention_desc& d, float* delta, int* status, cudaStream_t st, char* err) {
+int attn_masked_tc_bwd(const mslt_attention_desc& d, float* delta, int* next, int* status, cudaStream_t st, char* err) {
   TcParams p = params_of(d, status, attn_take_starve());
   MapVal mq[4], mk[4];
   const int loop_k = d.head_dim <= 64 ? BwdShape<64, true>::LOOP : BwdShape<128, true>::LOOP;
@@ -1330,8 +1343,10 @@ int attn_masked_tc_bwd(const mslt_attention_desc& d, float* delta, int* status, 
   while ((8 << log_lanes) < d.head_dim) log_lanes++;
   const long long rows = (long long)d.B * d.S * d.heads;
   launch_pdl(masked_delta_tc, (unsigned)(((rows << log_lanes) + 255) / 256), 256, 0, st, view_of(d.dctx), view_of(d.ctx), (const bf16*)d.rest,
-             delta, d.S, d.heads, d.head_dim, log_lanes, rows);
+             delta, next, d.S, d.heads, d.head_dim, log_lanes, rows);
   p.delta = pk.delta = delta;
+  p.next = next;
+  pk.next = next + 1;
   p.o0 = view_of(d.dq);
   p.wide = aligned32(d.dq);
   pk.o0 = view_of(d.dk);
