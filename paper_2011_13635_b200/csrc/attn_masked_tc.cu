@@ -819,10 +819,10 @@ static_assert(BwdShape<64, true>::ACC_COL + 2 * 64 <= 512 && BwdShape<128, false
 
 // kKeys = false: rows are queries (A = q, B = k, C = dctx, D = v; loop over keys), the result is dq.
 // kKeys = true: rows are keys (A = k, B = q, C = v, D = dctx; loop over the queries of every head that shares them): dk, dv.
-// Persistent, a block an SM: row tiles as they come (a counter: which block takes a tile changes no sum), steps counted on from tile to tile so that the barriers' phases go on.  The
-// producer warp works out a tile's list and asks for its rows while the tile before is under way; only the reading of
-// the accumulators lies between two tiles.  (8 x 12 x 2048 in 6 documents: a block a tile 344 us,
-// persistent blocks with tiles in turn 300, so 276.)
+// Persistent, a block an SM: row tiles as they come (from a counter: which block takes a tile changes no sum), steps counted on
+// from tile to tile so that the barriers' phases go on.  The producer warp works out a tile's list and asks for its rows while
+// the tile before is under way; only the reading of the accumulators lies between two tiles.  (8 x 12 x 2048 in 6 documents: a
+// block a tile 344 us, persistent blocks with tiles in turn 300, so 276.)
 template <int DP, bool kKeys, int kForm>
 __global__ void __launch_bounds__(AB_THREADS, 1)
 masked_bwd_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
